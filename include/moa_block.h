@@ -106,6 +106,31 @@ typedef struct {
 } moa_gemm_desc;
 moa_status moa_gemm(const moa_gemm_desc *desc, const void *A, const void *B, const void *R, void *C, void *stream);
 
+/* --------------------------------------------------------------- rotary positions
+ * Queries and keys turned by their positions, pair by pair of the first d_rot elements of each head:
+ *   angle = pos * inv_freq[i]      y1 = f (x1 cos - x2 sin)      y2 = f (x2 cos + x1 sin)      i = 0 .. d_rot/2 - 1
+ * MOA_ROPE_HALF pairs element i with i + d_rot/2, MOA_ROPE_PAIRS 2i with 2i + 1.  The elements from d_rot on are copied.  The angle
+ * is a product in 64 bits, reduced to a part of a turn before it is rounded, so that far positions keep their precision (and no table of
+ * them is needed: any int32 position).  inv_freq [d_rot/2] fp32 and the factor f hold whatever scaling a long context wants.  The
+ * gradient of x is the transposed rotation of the gradient of y, with the same factor: moa_rope_bwd.
+ * q, q_out: T tokens x H heads x d; k, k_out: T x H_k x d (H_k = 0: none, NULL); pos [T] int32.  Strides are {token, head} in elements
+ * ({0, 0}: contiguous [T,H,d]); each a multiple of 16 bytes and at least d, an output's rows must not overlap.  An output
+ * may be its own input (same address and strides); other overlaps are not allowed.  T, H >= 1; d a multiple of 8 up to 256;
+ * d_rot a multiple of 8, 8 <= d_rot <= d; dtype MOA_BF16 or MOA_F32 (fp32 arithmetic, rounded once).  HBM-bound: every element is read and written once. */
+typedef enum { MOA_ROPE_HALF = 0, MOA_ROPE_PAIRS = 1 } moa_rope_layout;
+typedef struct {
+    int32_t T, H, H_k, d, d_rot;
+    int32_t layout;          /* moa_rope_layout */
+    float   factor;
+    int32_t dtype;           /* moa_dtype of q, k, q_out, k_out */
+    int64_t q_stride[2], k_stride[2], q_out_stride[2], k_out_stride[2];
+} moa_rope_desc;
+moa_status moa_rope_fwd(const moa_rope_desc *desc, const int32_t *pos, const float *inv_freq, const void *q, const void *k,
+                        void *q_out, void *k_out, void *stream);
+/* Reads dq, dk (the gradients of q_out, k_out); writes dq_in, dk_in (those of q, k). */
+moa_status moa_rope_bwd(const moa_rope_desc *desc, const int32_t *pos, const float *inv_freq, const void *dq, const void *dk,
+                        void *dq_in, void *dk_in, void *stream);
+
 /* ---------------------------------------------------------------------- the block
  * A whole pre-norm transformer block as one call per direction: the sequence of the calls above with a packed Q/K/V
  * projection (host work only: a step of a small block spent more time between the calls than in them).

@@ -17,3 +17,4 @@ from .decode import decode_attn  # noqa: F401,E402
 from .block import (  # noqa: F401,E402
     rmsnorm_fwd_bwd, gated_mlp_fwd_bwd, gated_mlp_bwd_from_saved, gemm, transformer_block_fwd_bwd,
 )
+from . import cache  # noqa: F401,E402

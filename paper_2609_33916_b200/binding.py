@@ -1,4 +1,4 @@
-"""Binding of libmoa_attn.so (ctypes; the launching calls through _pycall): the same entry points as include/moa_attn.h.
+"""Binding of libmoa_attn.so (ctypes; the launching calls through _pycall): the same entry points as include/moa_attn.h, moa_block.h and moa_cache.h.
 
 Argument marshalling only -- every step of the attention path runs in the
 library's CUDA kernels.  Tensor arguments may be torch CUDA tensors (their
@@ -21,9 +21,11 @@ MOA_BF16, MOA_F32 = 0, 1
 MOA_DQ_AUTO, MOA_DQ_RED, MOA_DQ_BULK_REDUCE, MOA_DQ_SEPARATE_PASS = 0, 1, 2, 3
 MOA_PATH_AUTO, MOA_PATH_SIMT, MOA_PATH_TC = 0, 1, 2
 MOA_LAYOUT_BHND, MOA_LAYOUT_BNHD, MOA_LAYOUT_STRIDED = 0, 1, 2
+MOA_ROPE_HALF, MOA_ROPE_PAIRS = 0, 1
+MOA_CACHE_BF16, MOA_CACHE_INT4 = 0, 1
 MOA_OP_FWD, MOA_OP_BWD, MOA_OP_FUSED, MOA_OP_ROWPARALLEL = 0, 1, 2, 3
 
-#: every symbol include/moa_attn.h declares
+#: every symbol include/moa_attn.h and moa_block.h declare
 EXPORTS = (
     "moa_attn_workspace_bytes", "moa_attn_fwd", "moa_attn_bwd", "moa_attn_fused_fwd_bwd",
     "moa_last_device_status", "moa_launch_count", "moa_status_string", "moa_version",
@@ -31,8 +33,10 @@ EXPORTS = (
     "moa_decode_workspace_bytes", "moa_decode_attn",
     "moa_rmsnorm_workspace_bytes", "moa_rmsnorm_fwd", "moa_rmsnorm_bwd",
     "moa_gated_mlp_fwd", "moa_gated_mlp_workspace_bytes", "moa_gated_mlp_bwd", "moa_gemm", "moa_block_fwd", "moa_block_bwd",
-    "moa_selftest_expired_wait", "moa_bwd_pair_mode",
+    "moa_selftest_expired_wait", "moa_bwd_pair_mode", "moa_rope_fwd", "moa_rope_bwd",
 )
+#: those of include/moa_cache.h
+CACHE_EXPORTS = ("moa_cache_page_bytes", "moa_kv_append", "moa_kv_gather", "moa_paged_decode_workspace_bytes", "moa_paged_decode")
 
 
 class moa_attn_desc(ctypes.Structure):
@@ -70,6 +74,30 @@ class moa_block_arrays(ctypes.Structure):
                 ("x", "g1", "g2", "Wqkv", "Wo", "W1", "W3", "W2", "h1", "qkv", "o", "x2", "h2", "a", "u", "h", "y", "r1", "r2", "L",
                  "dy", "dh2", "dx2", "dout", "dqkv", "dh1", "dx", "dg1", "dg2", "dWqkv", "dWo", "dW1", "dW3", "dW2",
                  "norm_ws", "attn_ws", "mlp_ws")] + [(k, ctypes.c_size_t) for k in ("norm_ws_bytes", "attn_ws_bytes", "mlp_ws_bytes")]
+
+
+class moa_rope_desc(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("T", "H", "H_k", "d", "d_rot", "layout")] + [("factor", ctypes.c_float), ("dtype", ctypes.c_int32)] + [
+        (k, ctypes.c_int64 * 2) for k in ("q_stride", "k_stride", "q_out_stride", "k_out_stride")]
+
+
+class moa_cache_desc(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("pages", "page", "H_kv", "d", "format", "reserved")] + [("page_stride", ctypes.c_int64)]
+
+
+class moa_append_desc(ctypes.Structure):
+    _fields_ = [("cache", moa_cache_desc)] + [(k, ctypes.c_int32) for k in ("T", "H", "d_rot", "layout")] + [
+        ("factor", ctypes.c_float), ("dtype", ctypes.c_int32)] + [(k, ctypes.c_int64 * 2) for k in ("q_stride", "k_stride", "v_stride", "q_out_stride")]
+
+
+class moa_gather_desc(ctypes.Structure):
+    _fields_ = [("cache", moa_cache_desc), ("T", ctypes.c_int32), ("dtype", ctypes.c_int32), ("k_stride", ctypes.c_int64 * 2),
+                ("v_stride", ctypes.c_int64 * 2)]
+
+
+class moa_paged_decode_desc(ctypes.Structure):
+    _fields_ = [("cache", moa_cache_desc)] + [(k, ctypes.c_int32) for k in ("B", "H", "max_pages", "dtype")] + [
+        ("scale", ctypes.c_float), ("reserved", ctypes.c_int32), ("table_stride", ctypes.c_int64), ("q_stride", ctypes.c_int64 * 2)]
 
 
 MOA_KERNEL_KINDS = 6
@@ -133,6 +161,19 @@ def lib() -> ctypes.CDLL:
         for f in (L.moa_block_fwd, L.moa_block_bwd):
             f.restype = ctypes.c_int
             f.argtypes = [ctypes.POINTER(moa_block_desc), ctypes.POINTER(moa_block_arrays), vp]
+        for f in (L.moa_rope_fwd, L.moa_rope_bwd):
+            f.restype = ctypes.c_int
+            f.argtypes = [ctypes.POINTER(moa_rope_desc)] + [vp] * 6 + [vp]
+        L.moa_cache_page_bytes.restype = sz
+        L.moa_cache_page_bytes.argtypes = [ctypes.POINTER(moa_cache_desc)]
+        L.moa_kv_append.restype = ctypes.c_int
+        L.moa_kv_append.argtypes = [ctypes.POINTER(moa_append_desc)] + [vp] * 8 + [vp]
+        L.moa_kv_gather.restype = ctypes.c_int
+        L.moa_kv_gather.argtypes = [ctypes.POINTER(moa_gather_desc)] + [vp] * 4 + [vp]
+        L.moa_paged_decode_workspace_bytes.restype = sz
+        L.moa_paged_decode_workspace_bytes.argtypes = [ctypes.POINTER(moa_paged_decode_desc)]
+        L.moa_paged_decode.restype = ctypes.c_int
+        L.moa_paged_decode.argtypes = [ctypes.POINTER(moa_paged_decode_desc)] + [vp] * 7 + [sz, vp]
         L.moa_last_device_status.restype = ctypes.c_int
         L.moa_last_device_status.argtypes = [vp]
         L.moa_selftest_expired_wait.restype = ctypes.c_int
@@ -177,9 +218,12 @@ def strides_of(t):
 _ENTRIES = (("moa_attn_fwd", moa_attn_desc, 6, True), ("moa_attn_bwd", moa_attn_desc, 10, True),
             ("moa_attn_fused_fwd_bwd", moa_attn_desc, 10, True), ("moa_decode_attn", moa_decode_desc, 6, True),
             ("moa_rmsnorm_fwd", moa_rmsnorm_desc, 4, False), ("moa_rmsnorm_bwd", moa_rmsnorm_desc, 8, True), ("moa_gemm", moa_gemm_desc, 4, False),
-            ("moa_gated_mlp_fwd", moa_mlp_desc, 9, False), ("moa_gated_mlp_bwd", moa_mlp_desc, 13, True))
+            ("moa_gated_mlp_fwd", moa_mlp_desc, 9, False), ("moa_gated_mlp_bwd", moa_mlp_desc, 13, True),
+            ("moa_rope_fwd", moa_rope_desc, 6, False), ("moa_rope_bwd", moa_rope_desc, 6, False), ("moa_kv_append", moa_append_desc, 8, False),
+            ("moa_kv_gather", moa_gather_desc, 4, False), ("moa_paged_decode", moa_paged_decode_desc, 7, True))
 # their indexes in the extension's table, which outlives a reload of this module: set by _load, which runs before they are read
 _ATTN_FWD = _ATTN_BWD = _ATTN_FUSED = _DECODE = _NORM_FWD = _NORM_BWD = _GEMM = _MLP_FWD = _MLP_BWD = None
+_ROPE_FWD = _ROPE_BWD = _APPEND = _GATHER = _PAGED = None
 _invoke = _fill = None
 _load_lock = threading.Lock()
 
@@ -213,16 +257,19 @@ def _fill_ctypes(struct, objects):
 def _load():
     """_pycall.invoke, with the library's functions registered, or its form in ctypes where the extension is not there."""
     global _invoke, _fill, _ATTN_FWD, _ATTN_BWD, _ATTN_FUSED, _DECODE, _NORM_FWD, _NORM_BWD, _GEMM, _MLP_FWD, _MLP_BWD
+    global _ROPE_FWD, _ROPE_BWD, _APPEND, _GATHER, _PAGED
     with _load_lock:
         if _invoke is None:
             L = lib()
             try:
                 from . import _pycall
             except ImportError:          # not built for this interpreter: the same through ctypes
-                _ATTN_FWD, _ATTN_BWD, _ATTN_FUSED, _DECODE, _NORM_FWD, _NORM_BWD, _GEMM, _MLP_FWD, _MLP_BWD = range(len(_ENTRIES))
+                (_ATTN_FWD, _ATTN_BWD, _ATTN_FUSED, _DECODE, _NORM_FWD, _NORM_BWD, _GEMM, _MLP_FWD, _MLP_BWD, _ROPE_FWD, _ROPE_BWD, _APPEND,
+                 _GATHER, _PAGED) = range(len(_ENTRIES))
                 _fill, _invoke = _fill_ctypes, _invoke_ctypes
                 return _invoke
-            _ATTN_FWD, _ATTN_BWD, _ATTN_FUSED, _DECODE, _NORM_FWD, _NORM_BWD, _GEMM, _MLP_FWD, _MLP_BWD = (
+            (_ATTN_FWD, _ATTN_BWD, _ATTN_FUSED, _DECODE, _NORM_FWD, _NORM_BWD, _GEMM, _MLP_FWD, _MLP_BWD, _ROPE_FWD, _ROPE_BWD, _APPEND,
+             _GATHER, _PAGED) = (
                 _pycall.add_entry(ctypes.cast(getattr(L, name), ctypes.c_void_p).value, desc, pointers, ws) for name, desc, pointers, ws in _ENTRIES)
             _pycall.set_current_stream(lambda: _current_stream())
             _fill, _invoke = _pycall.fill, _pycall.invoke
@@ -430,6 +477,87 @@ def moa_decode_attn(desc, q, K, V, out, lse=None, ws=None, stream=None, ws_bytes
     s = (_invoke or _load())(_DECODE, desc, q, K, V, out, lse, ws, ws_bytes, stream)
     if check and s != MOA_OK:
         raise MoaError(s, "moa_decode_attn")
+    return s
+
+
+_CONTIGUOUS = (0, 0)
+
+
+def _pair(stride):
+    """A (token, head) stride in elements; None: contiguous."""
+    return (ctypes.c_int64 * 2)(*(_CONTIGUOUS if stride is None else (int(s) for s in stride)))
+
+
+def make_rope_desc(T, H, H_k, d, d_rot=None, layout=MOA_ROPE_HALF, factor=1.0, dtype=MOA_BF16, q_stride=None, k_stride=None, q_out_stride=None,
+                   k_out_stride=None) -> moa_rope_desc:
+    """T tokens, H query and H_k key heads (0: no keys) of d elements, the first d_rot of them (None: all) turned.  Strides: (token, head) in
+    elements, None: contiguous."""
+    return moa_rope_desc(int(T), int(H), int(H_k), int(d), int(d if d_rot is None else d_rot), int(layout), float(factor), int(dtype),
+                         _pair(q_stride), _pair(k_stride), _pair(q_out_stride), _pair(k_out_stride))
+
+
+def moa_rope_fwd(desc, pos, inv_freq, q, k, q_out, k_out, stream=None, check=True) -> int:
+    s = (_invoke or _load())(_ROPE_FWD, desc, pos, inv_freq, q, k, q_out, k_out, stream)
+    if check and s != MOA_OK:
+        raise MoaError(s, "moa_rope_fwd")
+    return s
+
+
+def moa_rope_bwd(desc, pos, inv_freq, dq, dk, dq_in, dk_in, stream=None, check=True) -> int:
+    """dq, dk: gradients of the rotated q, k; dq_in, dk_in: those of q, k."""
+    s = (_invoke or _load())(_ROPE_BWD, desc, pos, inv_freq, dq, dk, dq_in, dk_in, stream)
+    if check and s != MOA_OK:
+        raise MoaError(s, "moa_rope_bwd")
+    return s
+
+
+def make_cache_desc(pages, page, H_kv, d, format=MOA_CACHE_BF16, page_stride=0) -> moa_cache_desc:
+    """A pool of `pages` pages of `page` keys; page_stride in bytes (0: one after the other)."""
+    return moa_cache_desc(int(pages), int(page), int(H_kv), int(d), int(format), 0, int(page_stride))
+
+
+def moa_cache_page_bytes(desc) -> int:
+    return int(lib().moa_cache_page_bytes(ctypes.byref(desc)))
+
+
+def make_append_desc(cache, T, H, d_rot=None, layout=MOA_ROPE_HALF, factor=1.0, dtype=MOA_BF16, q_stride=None, k_stride=None, v_stride=None,
+                     q_out_stride=None) -> moa_append_desc:
+    """T tokens into `cache`; H query heads to turn beside the keys (0: none); d_rot None: the whole head."""
+    return moa_append_desc(cache, int(T), int(H), int(cache.d if d_rot is None else d_rot), int(layout), float(factor), int(dtype),
+                           _pair(q_stride), _pair(k_stride), _pair(v_stride), _pair(q_out_stride))
+
+
+def moa_kv_append(desc, q, k, v, pos, slot, inv_freq, q_out, pool, stream=None, check=True) -> int:
+    s = (_invoke or _load())(_APPEND, desc, q, k, v, pos, slot, inv_freq, q_out, pool, stream)
+    if check and s != MOA_OK:
+        raise MoaError(s, "moa_kv_append")
+    return s
+
+
+def make_gather_desc(cache, T, dtype=MOA_BF16, k_stride=None, v_stride=None) -> moa_gather_desc:
+    return moa_gather_desc(cache, int(T), int(dtype), _pair(k_stride), _pair(v_stride))
+
+
+def moa_kv_gather(desc, pool, slot, k, v, stream=None, check=True) -> int:
+    s = (_invoke or _load())(_GATHER, desc, pool, slot, k, v, stream)
+    if check and s != MOA_OK:
+        raise MoaError(s, "moa_kv_gather")
+    return s
+
+
+def make_paged_decode_desc(cache, B, H, max_pages, scale, dtype=MOA_BF16, table_stride=0, q_stride=None) -> moa_paged_decode_desc:
+    """B sequences, H query heads; tables of max_pages entries, table_stride entries apart (0: max_pages)."""
+    return moa_paged_decode_desc(cache, int(B), int(H), int(max_pages), int(dtype), float(scale), 0, int(table_stride), _pair(q_stride))
+
+
+def moa_paged_decode_workspace_bytes(desc) -> int:
+    return int(lib().moa_paged_decode_workspace_bytes(ctypes.byref(desc)))
+
+
+def moa_paged_decode(desc, q, pool, table, lens, out, lse=None, ws=None, stream=None, ws_bytes=None, check=True) -> int:
+    s = (_invoke or _load())(_PAGED, desc, q, pool, table, lens, out, lse, ws, ws_bytes, stream)
+    if check and s != MOA_OK:
+        raise MoaError(s, "moa_paged_decode")
     return s
 
 

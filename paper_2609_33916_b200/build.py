@@ -21,8 +21,8 @@ NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "--use_fast_math", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
-# the fp32 SIMT path is held to 1e-5 against the fp64 oracle: no fast-math there
-NO_FAST_MATH = {"simt_kernels.cu"}
+# the fp32 SIMT path is held to 1e-5 against the fp64 oracle, the rotations and the cache's codes to the nearest value: no fast-math there
+NO_FAST_MATH = {"simt_kernels.cu", "rope.cu", "cache.cu"}
 
 
 def _nvcc() -> str:

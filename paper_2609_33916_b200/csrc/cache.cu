@@ -1,0 +1,374 @@
+// The paged cache's append (rotation, rounding or quantisation, and the writes into the pages in one launch) and its read-back.
+//
+// HBM-bound: q is read and written once, k and v are read once and written as 2 or 0.5625 bytes per element.  As in rope.cu a block takes a few
+// tokens with all their rows (queries, keys, values), the angles of a token are made once and shared through shared memory, and a row is d / 16
+// lanes with two 16-byte pieces each, several rows in flight per lane.
+//
+// K is rounded to the nearest bf16 of the exact rotation.  In 32 bits the rotation is within 4e-7 (|x1| + |x2|) of it (two roundings of
+// products, the angle's, the factor's); where the two ends of that interval round apart, one element in about 3000, it is made again in 64 bits.
+// So what a key quantises to does not depend on which arithmetic turned it, and a 4-bit page is a function of the bf16 page's bits.
+//
+// Quantising: 32 neighbours share a scale s = bf16(amax / 7); x / s with one correction by the remainder is exact wherever the quotient is a tie
+// between two codes (x has 8 bits, the code and a half 4), so that halves go to even as the definition says.
+#include "cache_layout.cuh"
+
+namespace moa {
+namespace {
+
+using namespace ptx;
+
+constexpr int kThreads = 256, kTokens = 4, kUnroll = 2;
+using Piece = Chunk<__nv_bfloat16, 8>;
+
+struct AppendArgs {
+    const __nv_bfloat16 *q, *k, *v;
+    const int *pos;
+    const long long *slot;
+    const float *inv_freq;
+    __nv_bfloat16 *qo;
+    uint8_t *pool;
+    RopeStride sq, sk, sv, so;
+    long long page_stride, keys;     // keys: of the whole pool
+    int T, H, Hkv, page, d_rot, tt;
+    FastDiv rows;                    // H + 2 H_kv
+    float factor;
+};
+
+// The nearest bf16 of a double, in one rounding (half to even on the 45 bits that go); by way of float where the result has no normal bf16.
+__device__ __forceinline__ float round_bf16(double v)
+{
+    const double a = fabs(v);
+    if (!(a >= 0x1p-126 && a < 0x1.fep127)) return __bfloat162float(__float2bfloat16_rn((float)v));
+    long long b = __double_as_longlong(v);
+    b = (b + ((1LL << 44) - 1) + ((b >> 45) & 1)) & ~((1LL << 45) - 1);
+    return (float)__longlong_as_double(b);
+}
+
+// One element of a rotated pair in 64 bits, rounded to bf16: first: f (x1 cos - x2 sin), else f (x2 cos + x1 sin)
+__device__ __noinline__ float exact_turn(float x1, float x2, int pos, float f, float factor, bool first)
+{
+    double s, c;
+    sincos((double)pos * (double)f, &s, &c);
+    c *= (double)factor;
+    s *= (double)factor;
+    return round_bf16(first ? (double)x1 * c - (double)x2 * s : (double)x2 * c + (double)x1 * s);
+}
+
+// Of 16 elements of a lane (the lanes of a pair hold a group): codes of 1..15, four bits each in the order of the elements (the first lowest),
+// and the group's scale.
+__device__ __forceinline__ void quantise16(const float (&x)[16], uint32_t (&code)[2], uint16_t &scale)
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);      // (NaN is the largest)
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    const float amax = __uint_as_float(most);
+    float s = __bfloat162float(__float2bfloat16_rn(amax / 7.f));
+    const bool plain = most < 0x7f800000u && amax >= 0x1p-100f;
+    s = plain ? s : most >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : 0.f;
+    const float inv = plain ? 1.f / s : 0.f;
+    code[0] = code[1] = 0x88888888u;
+    if (plain) {
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            uint32_t c = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float v = x[8 * w + i], q0 = v * inv, q1 = fmaf(fmaf(-q0, s, v), inv, q0);
+                // adding 1.5 * 2^23 leaves the integer, rounded half to even, in the low bits
+                const int n = (int)(__float_as_uint(q1 + 12582912.f) - 0x4b400000u);
+                c |= (uint32_t)(min(max(n, -7), 7) + 8) << (4 * i);
+            }
+            code[w] = c;
+        }
+    }
+    scale = (uint16_t)(__float_as_uint(s) >> 16);
+}
+
+// Nibbles 0..7 (elements 8 t .. 8 t + 7 of a group) in the order of a word of K codes: the even elements, then the odd ones
+__device__ __forceinline__ uint32_t even_then_odd(uint32_t c)
+{
+    uint32_t e = c & 0x0f0f0f0fu, o = (c >> 4) & 0x0f0f0f0fu;
+    e = (e | (e >> 4)) & 0x00ff00ffu;
+    o = (o | (o >> 4)) & 0x00ff00ffu;
+    e = (e | (e >> 8)) & 0xffffu;
+    o = (o | (o >> 8)) & 0xffffu;
+    return e | (o << 16);
+}
+
+template <int D, bool kInt4, bool kPairs>
+__global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendArgs a)
+{
+    constexpr int kLanes = D / 16, kPer = kThreads / kLanes;
+    __shared__ float4 angles[kTokens * D / 4];
+    const int tid = threadIdx.x, lane = tid % 32, t0 = blockIdx.x * a.tt, nt = min(a.tt, a.T - t0), freqs = a.d_rot / 2, np = a.d_rot / 16;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int *pos = after_wait(a.pos);
+    const float *inv_freq = after_wait(a.inv_freq);
+    const long long *slots = after_wait(a.slot);
+    for (int i = tid; i < nt * freqs; i += kThreads) {
+        const int t = i / freqs, f = i - t * freqs;
+        float2 cs = position_angle(pos[t0 + t], inv_freq[f]);
+        cs.x *= a.factor;
+        cs.y *= a.factor;
+        write_angle<8>(angles + t * (freqs / 2), np, f, cs);
+    }
+    __syncthreads();
+    const int r0 = tid / kLanes, p = tid % kLanes, total = nt * (int)a.rows.d;
+    const bool turns = p < np;
+    const int c0 = turns && !kPairs ? 8 * p : 16 * p, c1 = turns && !kPairs ? freqs + 8 * p : c0 + 8;      // elements, for q and k; v: 16 p and 16 p + 8
+    const __nv_bfloat16 *q = after_wait(a.q), *k = after_wait(a.k), *v = after_wait(a.v);
+    // (all lanes of a warp make the same rounds: the exchanges below are of whole warps)
+    for (int base = (int)blockIdx.y * kPer * kUnroll; base < total; base += kPer * kUnroll * (int)gridDim.y) {
+        Piece x[kUnroll], y[kUnroll];
+        int tok[kUnroll], head[kUnroll], kind[kUnroll];      // kind 0 q, 1 k, 2 v, -1 none
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int row = base + r0 + u * kPer;
+            kind[u] = -1;
+            tok[u] = head[u] = 0;
+            x[u].w = y[u].w = make_uint4(0u, 0u, 0u, 0u);
+            if (row < total) {
+                tok[u] = (int)a.rows.div((uint32_t)row);
+                const int h = row - tok[u] * (int)a.rows.d;
+                const long long t = t0 + tok[u];
+                kind[u] = h < a.H ? 0 : h < a.H + a.Hkv ? 1 : 2;
+                head[u] = kind[u] == 0 ? h : kind[u] == 1 ? h - a.H : h - a.H - a.Hkv;
+                const __nv_bfloat16 *src = kind[u] == 0   ? q + t * a.sq.token + head[u] * a.sq.head
+                                           : kind[u] == 1 ? k + t * a.sk.token + head[u] * a.sk.head
+                                                          : v + t * a.sv.token + head[u] * a.sv.head;
+                x[u].w = *reinterpret_cast<const uint4 *>(src + (kind[u] == 2 ? 16 * p : c0));
+                y[u].w = *reinterpret_cast<const uint4 *>(src + (kind[u] == 2 ? 16 * p + 8 : c1));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            float fx[8], fy[8];
+            x[u].unpack(fx);
+            y[u].unpack(fy);
+            if ((kind[u] == 0 || kind[u] == 1) && turns) {
+                float c[8], s[8], gx[8], gy[8];
+                read_angles<8>(angles + tok[u] * (freqs / 2), np, p, c, s);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { gx[i] = fx[i]; gy[i] = fy[i]; }
+                rotate<8, kPairs>(fx, fy, c, s);
+                if (kind[u] == 1) {
+                    const float off = 4e-7f * fabsf(a.factor);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float x1 = kPairs ? (i < 4 ? gx[2 * i] : gy[2 * i - 8]) : gx[i], x2 = kPairs ? (i < 4 ? gx[2 * i + 1] : gy[2 * i - 7]) : gy[i];
+                        float &y1 = kPairs ? (i < 4 ? fx[2 * i] : fy[2 * i - 8]) : fx[i], &y2 = kPairs ? (i < 4 ? fx[2 * i + 1] : fy[2 * i - 7]) : fy[i];
+                        const float e = off * (fabsf(x1) + fabsf(x2));
+                        const uint32_t lo = pack_bf16(y1 - e, y2 - e), hi = pack_bf16(y1 + e, y2 + e);
+                        if (lo != hi) {
+                            const int at = pos[t0 + tok[u]];
+                            const float f = inv_freq[8 * p + i];
+                            y1 = exact_turn(x1, x2, at, f, a.factor, true);
+                            y2 = exact_turn(x1, x2, at, f, a.factor, false);
+                        }
+                    }
+                }
+                x[u].pack(fx);
+                y[u].pack(fy);
+            }
+            if (kind[u] == 0) {
+                __nv_bfloat16 *dst = a.qo + (long long)(t0 + tok[u]) * a.so.token + head[u] * a.so.head;
+                *reinterpret_cast<uint4 *>(dst + c0) = x[u].w;
+                *reinterpret_cast<uint4 *>(dst + c1) = y[u].w;
+            }
+            long long at = -1;
+            if (kind[u] > 0) at = slots[t0 + tok[u]];
+            const bool there = at >= 0 && at < a.keys;
+            const long long pg = there ? at / a.page : 0;
+            const int key = there ? (int)(at - pg * a.page) : 0;
+            uint8_t *page = a.pool + pg * a.page_stride;
+            if constexpr (!kInt4) {
+                if (there) {
+                    uint8_t *dst = page + row16(a.page, D, head[u], kind[u] - 1, key);
+                    *reinterpret_cast<uint4 *>(dst + 2 * (kind[u] == 2 ? 16 * p : c0)) = x[u].w;
+                    *reinterpret_cast<uint4 *>(dst + 2 * (kind[u] == 2 ? 16 * p + 8 : c1)) = y[u].w;
+                }
+            } else {
+                if (!__any_sync(0xffffffffu, kind[u] > 0)) continue;
+                // the half layout's lanes hold pieces p and p + d_rot / 16: each gets pieces 2 p and 2 p + 1 from the lanes that have them
+                if (!kPairs && __any_sync(0xffffffffu, kind[u] == 1) && np > 0) {
+                    uint4 got[2];
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        const int piece = 2 * p + w, from = lane - p + (piece < 2 * np ? piece % np : p);
+                        const bool second = piece < 2 * np && piece >= np;
+                        const uint32_t xs[4] = {x[u].w.x, x[u].w.y, x[u].w.z, x[u].w.w}, ys[4] = {y[u].w.x, y[u].w.y, y[u].w.z, y[u].w.w};
+                        uint32_t g[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t gx = __shfl_sync(0xffffffffu, xs[i], from), gy = __shfl_sync(0xffffffffu, ys[i], from);
+                            g[i] = second ? gy : gx;
+                        }
+                        got[w] = make_uint4(g[0], g[1], g[2], g[3]);
+                    }
+                    if (kind[u] == 1 && turns) { x[u].w = got[0]; y[u].w = got[1]; }
+                }
+                x[u].unpack(fx);
+                y[u].unpack(fy);
+                float e[16];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { e[i] = fx[i]; e[8 + i] = fy[i]; }
+                uint32_t code[2];
+                uint16_t scale;
+                quantise16(e, code, scale);
+                const int y0 = p / 2, half = p % 2, r = key % kBlockKeys;      // group, and which 16 of it
+                uint8_t *blk = page + block4<D>(a.page, head[u], key / kBlockKeys);
+                using L = Block4<D>;
+                // V: a word holds four elements of two neighbouring groups: the lanes of those trade halves of their codes
+                const uint32_t trade = __shfl_xor_sync(0xffffffffu, code[y0 % 2 ? 0 : 1], 2);
+                if (there && kind[u] == 1) {
+                    *reinterpret_cast<uint32_t *>(blk + L::k_word(r, 2 * half, y0)) = even_then_odd(code[0]);
+                    *reinterpret_cast<uint32_t *>(blk + L::k_word(r, 2 * half + 1, y0)) = even_then_odd(code[1]);
+                    if (half == 0) *reinterpret_cast<uint16_t *>(blk + L::k_scale(r, y0)) = scale;
+                }
+                if (there && kind[u] == 2) {
+                    const uint32_t mine = code[y0 % 2 ? 1 : 0], even = y0 % 2 ? trade : mine, odd = y0 % 2 ? mine : trade;
+                    const int g = 4 * half + (y0 % 2 ? 2 : 0);
+                    *reinterpret_cast<uint32_t *>(blk + L::v_word(r, g, y0 / 2)) = (even & 0xffffu) | (odd << 16);
+                    *reinterpret_cast<uint32_t *>(blk + L::v_word(r, g + 1, y0 / 2)) = (even >> 16) | (odd & 0xffff0000u);
+                    if (half == 0) *reinterpret_cast<uint16_t *>(blk + L::v_scale(r, y0)) = scale;
+                }
+            }
+        }
+    }
+}
+
+struct GatherArgs {
+    const uint8_t *pool;
+    const long long *slot;
+    void *k, *v;
+    RopeStride sk, sv;
+    long long page_stride, keys, rows;     // rows: T * 2 H_kv
+    int Hkv, page;
+};
+
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&f)[8])
+{
+    Piece x;
+    x.pack(f);
+    *reinterpret_cast<uint4 *>(p) = x.w;
+}
+__device__ __forceinline__ void store8(float *p, const float (&f)[8])
+{
+    reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+}
+
+// A row of a head is d / 8 lanes with 8 elements each; rows in the order token, K or V, head
+template <typename T, int D, bool kInt4>
+__global__ void __launch_bounds__(kThreads) kv_gather_kernel(const GatherArgs a)
+{
+    constexpr int kLanes = D / 8;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const uint8_t *pool = after_wait(a.pool);
+    const long long *slots = after_wait(a.slot);
+    const int c = threadIdx.x % kLanes;
+    const long long step = (long long)gridDim.x * (kThreads / kLanes);
+    for (long long row = (long long)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes; row < a.rows; row += step) {
+        const long long t = row / (2 * a.Hkv);
+        const int rest = (int)(row - t * 2 * a.Hkv), v = rest >= a.Hkv, h = rest - v * a.Hkv;
+        const long long at = slots[t];
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = 0.f;
+        if (at >= 0 && at < a.keys) {
+            const long long pg = at / a.page;
+            const int key = (int)(at - pg * a.page), r = key % kBlockKeys;
+            const uint8_t *page = pool + pg * a.page_stride;
+            if constexpr (!kInt4) {
+                Piece x;
+                x.w = *reinterpret_cast<const uint4 *>(page + row16(a.page, D, h, v, key) + 16 * c);
+                x.unpack(f);
+            } else {
+                using L = Block4<D>;
+                const uint8_t *blk = page + block4<D>(a.page, h, key / kBlockKeys);
+                const int y = c / 4, t8 = c % 4;
+                uint32_t code;       // eight nibbles in the order of the elements
+                if (v) {
+                    const int sh = 16 * (y % 2);
+                    const uint32_t lo = *reinterpret_cast<const uint32_t *>(blk + L::v_word(r, 2 * t8, y / 2));
+                    const uint32_t hi = *reinterpret_cast<const uint32_t *>(blk + L::v_word(r, 2 * t8 + 1, y / 2));
+                    code = ((lo >> sh) & 0xffffu) | ((hi >> sh) << 16);
+                } else {
+                    code = *reinterpret_cast<const uint32_t *>(blk + L::k_word(r, t8, y));
+                }
+                const float s = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(blk + (v ? L::v_scale(r, y) : L::k_scale(r, y))) << 16);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int n = v ? i : 4 * (i % 2) + i / 2;
+                    f[i] = s * (float)((int)((code >> (4 * n)) & 15u) - 8);
+                }
+            }
+        }
+        T *dst = v ? (T *)a.v + t * a.sv.token + h * a.sv.head : (T *)a.k + t * a.sk.token + h * a.sk.head;
+        store8(dst + 8 * c, f);
+    }
+}
+
+template <int D, bool kInt4>
+cudaError_t launch_append(const AppendArgs &a, bool pairs, dim3 grid, cudaStream_t st)
+{
+    LaunchScope scope(MOA_KERNEL_OTHER, st);
+    return pairs ? launch_dependent(kv_append_kernel<D, kInt4, true>, grid, dim3(kThreads), (size_t)0, st, a)
+                 : launch_dependent(kv_append_kernel<D, kInt4, false>, grid, dim3(kThreads), (size_t)0, st, a);
+}
+
+template <typename T>
+cudaError_t launch_gather(const GatherArgs &a, int d, int int4, cudaStream_t st)
+{
+    const long long per = kThreads / (d / 8), want = (a.rows + per - 1) / per, most = 32LL * device_info().sms;
+    const dim3 grid((unsigned)(want < most ? want : most));
+    LaunchScope scope(MOA_KERNEL_OTHER, st);
+    if (d == 64)
+        return int4 ? launch_dependent(kv_gather_kernel<T, 64, true>, grid, dim3(kThreads), (size_t)0, st, a)
+                    : launch_dependent(kv_gather_kernel<T, 64, false>, grid, dim3(kThreads), (size_t)0, st, a);
+    return int4 ? launch_dependent(kv_gather_kernel<T, 128, true>, grid, dim3(kThreads), (size_t)0, st, a)
+                : launch_dependent(kv_gather_kernel<T, 128, false>, grid, dim3(kThreads), (size_t)0, st, a);
+}
+
+}  // namespace
+
+cudaError_t kv_append(const AppendProblem &p, const void *q, const void *k, const void *v, const int *pos, const long long *slot,
+                      const float *inv_freq, void *qo, void *pool, cudaStream_t st)
+{
+    AppendArgs a{};
+    a.q = (const __nv_bfloat16 *)q; a.k = (const __nv_bfloat16 *)k; a.v = (const __nv_bfloat16 *)v;
+    a.pos = pos; a.slot = slot; a.inv_freq = inv_freq; a.qo = (__nv_bfloat16 *)qo; a.pool = (uint8_t *)pool;
+    a.sq = p.sq; a.sk = p.sk; a.sv = p.sv; a.so = p.so;
+    a.page_stride = p.pool.page_stride;
+    a.keys = (long long)p.pool.pages * p.pool.page;
+    a.T = p.T; a.H = p.H; a.Hkv = p.pool.Hkv; a.page = p.pool.page; a.d_rot = p.d_rot;
+    a.rows = FastDiv((uint32_t)(p.H + 2 * p.pool.Hkv));
+    a.factor = p.factor;
+    const int per = kThreads / (p.pool.d / 16), sms = device_info().sms;
+    a.tt = kTokens;
+    while (a.tt > 1 && (p.T + a.tt - 1) / a.tt < 4 * sms) a.tt /= 2;
+    const int blocks = (p.T + a.tt - 1) / a.tt;
+    const long long passes = ((long long)a.tt * (int)a.rows.d + per * kUnroll - 1) / (per * kUnroll);
+    int split = 1;
+    while (split < passes && (long long)blocks * split < 2 * sms) ++split;
+    const dim3 grid((unsigned)blocks, (unsigned)split);
+    if (p.pool.d == 64) return p.pool.int4 ? launch_append<64, true>(a, p.pairs, grid, st) : launch_append<64, false>(a, p.pairs, grid, st);
+    return p.pool.int4 ? launch_append<128, true>(a, p.pairs, grid, st) : launch_append<128, false>(a, p.pairs, grid, st);
+}
+
+cudaError_t kv_gather(const CachePool &pool, int T, int dtype, const void *base, const long long *slot, void *k, void *v, RopeStride sk, RopeStride sv,
+                      cudaStream_t st)
+{
+    GatherArgs a{};
+    a.pool = (const uint8_t *)base; a.slot = slot; a.k = k; a.v = v; a.sk = sk; a.sv = sv;
+    a.page_stride = pool.page_stride;
+    a.keys = (long long)pool.pages * pool.page;
+    a.rows = 2LL * T * pool.Hkv;
+    a.Hkv = pool.Hkv; a.page = pool.page;
+    return dtype == MOA_F32 ? launch_gather<float>(a, pool.d, pool.int4, st) : launch_gather<__nv_bfloat16>(a, pool.d, pool.int4, st);
+}
+
+}  // namespace moa

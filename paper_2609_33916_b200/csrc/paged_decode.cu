@@ -1,0 +1,672 @@
+// Decode attention over a paged cache, bf16 or 4 bits: one new query per head, a table of pages and a length per sequence.
+//
+//   out = softmax(scale q K^T) V      S^T = K q^T and O^T = V^T P^T on mma.sync m16n8k16, 16 keys (16 elements of d) as its rows and the up
+//                                     to eight queries of a K/V head as its columns
+//
+// HBM-bound: 4 d (bf16) or 1.125 d (4 bits) bytes per key and K/V head.  Keys as the rows of the tile: a group of up to eight queries costs
+// one product per 256 elements of the cache, half of what the queries as 16 rows would (groups of 9 to 16: two).  What bounds the 4-bit form beside the
+// bytes is its instructions: an SM has about 400 issue slots in the time HBM takes for 16 keys of a head at d = 128 (2304 bytes).  So
+//   * codes become bf16 by one mask-and-or: 0x4300 | c is 128 + c.  K: the 136 too many are taken off in the products' starting value,
+//     -136 sum(q) of the group; V: by one packed subtraction, exact;
+//   * K's scale multiplies the products of a group of 32, in fp32; V's is multiplied into the weights (bf16, as the weights of the products are);
+//   * the page's layout (cache_layout.cuh) is the one in which a lane's codes and scales are 16-byte words: no exchange of any kind.
+// A warp streams 16 keys at a time through a ring of its own in shared memory (cp.async; no barrier among warps), with the table entries of
+// its next 32 steps in a register of each lane, fetched a batch ahead.
+//
+// Work split: a unit is 64 keys of a K/V head (16 per warp of a CTA).  All units of all sequences, in the order sequence, head, key, are cut into
+// equal shares, one per resident CTA, on the device (the host does not know the lengths): every CTA adds up the lengths and finds its
+// share.  A head that lies in one share is written at once; the others leave partial results (at most two per CTA) and a merge kernel, set up meanwhile,
+// joins them: CTA c tells it which head begins in its share and goes on, and where that ends.
+#include "cache_layout.cuh"
+#include "ptx.cuh"
+
+namespace moa {
+namespace {
+
+using namespace ptx;
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kUnitKeys = 16 * kWarps;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kRescale = 8.f;      // weights may exceed 1 by this power of two before the sums are scaled again
+
+struct PagedArgs {
+    const __nv_bfloat16 *q;
+    const uint8_t *pool;
+    const int *table, *lens;
+    __nv_bfloat16 *out;
+    float *lse, *part_o, *part_ml;
+    int2 *info;                 // per CTA: the head that begins in its share and goes on (-1: none), the CTA that ends it
+    RopeStride sq;
+    long long table_stride, page_stride;
+    int B, Hkv, G, pages, page, cap;      // cap: keys that a row of the table has room for
+    FastDiv by_page;
+    float scale_log2;
+};
+
+template <int D, bool kInt4, int NQ>
+struct Cfg {
+    static constexpr int kStage = kInt4 ? Block4<D>::kBytes : 16 * D * 4;
+    static constexpr int kCtas = NQ == 2 ? 2 : kInt4 ? 4 : D == 128 ? 2 : 3;          // resident per SM
+    static constexpr int kStages = kInt4 ? (D == 128 ? (NQ == 2 ? 8 : 4) : 8) : D == 128 ? 3 : 4;
+    static constexpr int kLd = D + 4;                                                  // floats of a row of the merge
+    static constexpr int offMerge = kWarps * kStages * kStage;
+    static constexpr int offMl = offMerge + kWarps * 8 * kLd * 4;                      // [warps][8] (maximum, sum)
+    static constexpr int offScan = offMl + kWarps * 8 * 8;
+    static constexpr int kTotal = offScan + 64;
+    static constexpr int kNO = D / 16;                                                 // tiles of O^T
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint4 lds128(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Two codes as bf16: 128 + c each (nibbles i and 4 + i of w)
+__device__ __forceinline__ uint32_t codes128(uint32_t w, int i) { return ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u; }
+__device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+__device__ __forceinline__ int units_of(int len) { return len > 0 ? (len + kUnitKeys - 1) / kUnitKeys : 1; }
+__device__ __forceinline__ int first_unit(int units, int c, int ctas) { return (int)((long long)units * c / ctas); }
+
+// The share of CTA c: units [u0, u1) of `units`, and the sequence that holds u0 with the units in front of it
+struct Share {
+    int units, ctas, u0, u1, b, before;
+};
+__device__ __forceinline__ Share find_share(const PagedArgs &a, const int *lens, int *scan)
+{
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    Share s;
+    int sum = 0, first = 0;
+    for (int b = tid; b < a.B; b += kThreads) {
+        const int n = units_of(min(lens[b], a.cap));
+        if (b == tid) first = n;
+        sum += n;
+    }
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) scan[warp] = sum;
+    __syncthreads();
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) sum += scan[w];
+    s.units = sum * a.Hkv;
+    s.ctas = min((int)gridDim.x, s.units);
+    const int c = blockIdx.x;
+    s.u0 = c < s.ctas ? first_unit(s.units, c, s.ctas) : s.units;
+    s.u1 = c < s.ctas ? first_unit(s.units, c + 1, s.ctas) : s.units;
+    s.b = s.before = 0;
+    if (s.u0 == s.u1) return s;
+    const int row = s.u0 / a.Hkv;      // units of one head: the sequence is the one whose sum passes this (all heads have the same)
+    int carry = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+        const int b = b0 + tid, n = b0 == 0 ? first : b < a.B ? units_of(min(lens[b], a.cap)) : 0;
+        int incl = n;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        __syncthreads();
+        if (lane == 31) scan[warp] = incl;
+        __syncthreads();
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) incl += scan[w];
+            all += scan[w];
+        }
+        incl += carry;
+        if (incl - n <= row && row < incl) { scan[4] = b; scan[5] = incl - n; }
+        carry += all;
+        if (carry > row) break;      // (the same in every thread)
+    }
+    __syncthreads();
+    s.b = scan[4];
+    s.before = scan[5] * a.Hkv;
+    return s;
+}
+
+// A place in a share: unit t of head h of sequence b, whose length is len
+struct Place {
+    int b, h, t, len, end;      // end: units of a head of the sequence
+    __device__ __forceinline__ void set(int seq, int head, int unit, int n)
+    {
+        b = seq; h = head; t = unit; len = n; end = units_of(n);
+    }
+};
+
+template <int D, bool kInt4, int NQ>
+__global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_decode_kernel(const PagedArgs a)
+{
+    using C = Cfg<D, kInt4, NQ>;
+    constexpr int kG = D / 32, S = C::kStages;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    float *merge = reinterpret_cast<float *>(smem + C::offMerge);
+    float2 *ml = reinterpret_cast<float2 *>(smem + C::offMl);
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, t4 = lane % 4;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int *lens = after_wait(a.lens), *table = after_wait(a.table);
+    const uint8_t *pool = after_wait(a.pool);
+    const __nv_bfloat16 *q = after_wait(a.q);
+    const Share sh = find_share(a, lens, reinterpret_cast<int *>(smem + C::offScan));
+    auto length = [&](int b) { return b < a.B ? max(0, min(lens[b], a.cap)) : 0; };
+    int count = sh.u1 - sh.u0;
+    if (count == 0) {
+        if (tid == 0) a.info[blockIdx.x] = make_int2(-1, 0);
+        return;
+    }
+    Place use;
+    {
+        const int len = length(sh.b), end = units_of(len), in = sh.u0 - sh.before;
+        use.set(sh.b, in / end, in % end, len);
+    }
+
+    // ---- requests: S - 1 steps ahead of their use
+    const uint32_t ring = smem_u32(smem) + warp * S * C::kStage;
+    Place ask = use;
+    int asked = 0, base = ask.t;      // base: unit of the batch's first entry
+    uint32_t live = 0;                // stages that hold keys
+    // where 16 keys of unit t + lane of head h of sequence b begin (their block, or their row of K), as an offset from the pool; -1: no such page
+    auto entry = [&](int b, int h, int t) -> long long {
+        const int key = (t + lane) * kUnitKeys + 16 * warp;
+        if (key >= a.cap || b >= a.B) return -1;
+        const int at = (int)a.by_page.div((uint32_t)key), in = key - at * a.page, pg = table[b * a.table_stride + at];
+        if ((unsigned)pg >= (unsigned)a.pages) return -1;
+        return pg * a.page_stride + (kInt4 ? block4<D>(a.page, h, in / kBlockKeys) : row16(a.page, D, h, 0, in));
+    };
+    long long cur = entry(ask.b, ask.h, ask.t), nxt;
+    int nlen;
+    Place np;
+    auto fetch_next = [&] {      // the batch behind the current one
+        np = ask;
+        if (base + 32 < ask.end) {
+            np.t = base + 32;
+            nlen = ask.len;
+        } else {
+            np.t = 0;
+            if (++np.h == a.Hkv) { np.h = 0; ++np.b; }
+            nlen = np.b == ask.b ? ask.len : length(np.b);
+        }
+        nxt = entry(np.b, np.h, np.t);
+    };
+    fetch_next();
+    auto request = [&] {
+        if (asked < count) {
+            const long long at = __shfl_sync(0xffffffffu, cur, ask.t - base);
+            const int key0 = ask.t * kUnitKeys + 16 * warp, left = ask.len - key0;
+            const uint32_t dst = ring + asked % S * C::kStage;
+            live &= ~(1u << (asked % S));
+            if (at >= 0 && left > 0) {
+                live |= 1u << (asked % S);
+                const uint8_t *src = pool + at;
+                if constexpr (kInt4) {
+                    constexpr int kPieces = C::kStage / 16;
+#pragma unroll
+                    for (int i = 0; i < (kPieces + 31) / 32; ++i)
+                        if (i * 32 + 32 <= kPieces || i * 32 + lane < kPieces) cp_async16(dst + 16 * (32 * i + lane), src + 16 * (32 * i + lane), 16);
+                } else {
+                    // rows past the end of the sequence are filled with zeros: whatever they hold, their weight is 0
+                    constexpr int kRow = D / 8, kAt = 32 / kRow;
+                    const int c = lane % kRow;
+#pragma unroll
+                    for (int i = 0; i < 16 / kAt; ++i) {
+                        const int r = i * kAt + lane / kRow, bytes = r < left ? 16 : 0;
+                        const uint32_t to = dst + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16;
+                        const uint8_t *from = src + (bytes ? r * (2 * D) + c * 16 : 0);
+                        cp_async16(to, from, bytes);
+                        cp_async16(to + 32 * D, from + (long long)a.page * (2 * D), bytes);
+                    }
+                }
+            }
+            ++asked;
+            if (++ask.t == ask.end) {
+                ask.set(np.b, np.h, 0, nlen);
+                base = 0;
+                cur = nxt;
+                fetch_next();
+            } else if (ask.t == base + 32) {
+                base += 32;
+                cur = nxt;
+                fetch_next();
+            }
+        }
+        cp_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) request();
+
+    // ---- use
+    int done = 0;
+    int2 told = make_int2(-1, 0);
+    while (done < count) {
+        const int first = use.t, steps = min(use.end - use.t, count - done), head = use.b * a.Hkv + use.h;
+        // the group's queries: B operands, and 4 bits: the products' starting values
+        uint32_t qf[NQ][kInt4 ? 4 * kG : D / 8];
+        float bias[NQ][kInt4 ? kG : 1][2];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const int row = 8 * n + g;
+            const __nv_bfloat16 *src = q + use.b * a.sq.token + (long long)(use.h * a.G + row) * a.sq.head;
+            if constexpr (kInt4) {
+#pragma unroll
+                for (int y = 0; y < kG; ++y) {
+                    const uint4 v = row < a.G ? *reinterpret_cast<const uint4 *>(src + 32 * y + 8 * t4) : make_uint4(0u, 0u, 0u, 0u);
+                    qf[n][4 * y] = v.x; qf[n][4 * y + 1] = v.y; qf[n][4 * y + 2] = v.z; qf[n][4 * y + 3] = v.w;
+                    float s = ((low_bf16(v.x) + high_bf16(v.x)) + (low_bf16(v.y) + high_bf16(v.y))) + ((low_bf16(v.z) + high_bf16(v.z)) + (low_bf16(v.w) + high_bf16(v.w)));
+                    s += __shfl_xor_sync(0xffffffffu, s, 1);
+                    s += __shfl_xor_sync(0xffffffffu, s, 2);
+                    s *= -136.f;
+                    bias[n][y][0] = __shfl_sync(0xffffffffu, s, 8 * t4);
+                    bias[n][y][1] = __shfl_sync(0xffffffffu, s, 8 * t4 + 4);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) qf[n][i] = row < a.G ? *reinterpret_cast<const uint32_t *>(src + 8 * i + 2 * t4) : 0u;
+            }
+        }
+        float o[NQ][C::kNO][4], m[NQ][2], l[NQ][2];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            m[n][0] = m[n][1] = -INFINITY;
+            l[n][0] = l[n][1] = 0.f;
+#pragma unroll
+            for (int i = 0; i < C::kNO; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][i][e] = 0.f;
+        }
+        for (int step = 0; step < steps; ++step, ++done, ++use.t) {
+            cp_wait<S - 2>();
+            __syncwarp();
+            request();
+            const int key0 = use.t * kUnitKeys + 16 * warp, left = use.len - key0;
+            if (!((live >> (done % S)) & 1u)) continue;
+            const uint32_t st = ring + done % S * C::kStage;
+            float sc[NQ][4];
+            if constexpr (kInt4) {
+                // rows g and g + 8 of the tile are keys; a lane's words are eight elements of each group
+                uint32_t k0[kG], k1[kG], ks[kG];
+                if constexpr (D == 128) {
+                    const uint4 x = lds128(st + g * 64 + t4 * 16), y = lds128(st + (g + 8) * 64 + t4 * 16), z = lds128(st + Block4<D>::offKS + g * 16);
+                    k0[0] = x.x; k0[1] = x.y; k0[2] = x.z; k0[3] = x.w;
+                    k1[0] = y.x; k1[1] = y.y; k1[2] = y.z; k1[3] = y.w;
+                    ks[0] = z.x; ks[1] = z.y; ks[2] = z.z; ks[3] = z.w;
+                } else {
+                    const uint2 x = lds64(st + g * 32 + t4 * 8), y = lds64(st + (g + 8) * 32 + t4 * 8), z = lds64(st + Block4<D>::offKS + g * 8);
+                    k0[0] = x.x; k0[1] = x.y;
+                    k1[0] = y.x; k1[1] = y.y;
+                    ks[0] = z.x; ks[1] = z.y;
+                }
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
+#pragma unroll
+                for (int y = 0; y < kG; ++y) {
+                    uint32_t lo[4], hi[4];
+                    lo[0] = codes128(k0[y], 0); lo[1] = codes128(k1[y], 0); lo[2] = codes128(k0[y], 1); lo[3] = codes128(k1[y], 1);
+                    hi[0] = codes128(k0[y], 2); hi[1] = codes128(k1[y], 2); hi[2] = codes128(k0[y], 3); hi[3] = codes128(k1[y], 3);
+                    // scales: words [row g: groups 0 1, 2 3][row g + 8: 0 1, 2 3]
+                    const uint32_t w0 = ks[y / 2], w1 = ks[kG / 2 + y / 2];
+                    const float s0 = y % 2 ? high_bf16(w0) : low_bf16(w0), s1 = y % 2 ? high_bf16(w1) : low_bf16(w1);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) {
+                        float c[4] = {bias[n][y][0], bias[n][y][1], bias[n][y][0], bias[n][y][1]};
+                        mma16816(c, lo, qf[n][4 * y], qf[n][4 * y + 1]);
+                        mma16816(c, hi, qf[n][4 * y + 2], qf[n][4 * y + 3]);
+                        sc[n][0] = fmaf(s0, c[0], sc[n][0]);
+                        sc[n][1] = fmaf(s0, c[1], sc[n][1]);
+                        sc[n][2] = fmaf(s1, c[2], sc[n][2]);
+                        sc[n][3] = fmaf(s1, c[3], sc[n][3]);
+                    }
+                }
+            } else {
+                float odd[NQ][4];
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[n][e] = odd[n][e] = 0.f;
+                const int r = (lane / 8 & 1) * 8 + lane % 8;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const int c = 2 * i + lane / 16;
+                    uint32_t ka[4];
+                    ldmatrix4(ka, st + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) mma16816(i % 2 ? odd[n] : sc[n], ka, qf[n][2 * i], qf[n][2 * i + 1]);
+                }
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[n][e] += odd[n][e];
+            }
+            bool grow = false;
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sc[n][e] *= a.scale_log2;
+                    if (left < 16 && g + 8 * (e / 2) >= left) sc[n][e] = -INFINITY;
+                }
+                grow = grow || fmaxf(sc[n][0], sc[n][2]) > m[n][0] + kRescale || fmaxf(sc[n][1], sc[n][3]) > m[n][1] + kRescale;
+            }
+            if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float mx = fmaxf(sc[n][e], sc[n][2 + e]);
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                        mx = fmaxf(mx, m[n][e]);
+                        const float f = mx == -INFINITY ? 1.f : ex2(m[n][e] - mx);
+                        m[n][e] = mx;
+                        l[n][e] *= f;
+#pragma unroll
+                        for (int i = 0; i < C::kNO; ++i) { o[n][i][e] *= f; o[n][i][2 + e] *= f; }
+                    }
+            }
+            uint32_t pb[NQ][2];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                const float r0 = m[n][0] == -INFINITY ? 0.f : m[n][0], r1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
+                const float p0 = ex2(sc[n][0] - r0), p1 = ex2(sc[n][1] - r1), p2 = ex2(sc[n][2] - r0), p3 = ex2(sc[n][3] - r1);
+                l[n][0] += p0 + p2;
+                l[n][1] += p1 + p3;
+                pb[n][0] = transpose8(pack_bf16(p0, p1));
+                pb[n][1] = transpose8(pack_bf16(p2, p3));
+            }
+            if constexpr (kInt4) {
+                uint32_t va[D / 64][4], vs[kG][2];      // [h][key 2 t, 2 t + 1, 2 t + 8, 2 t + 9]
+                const uint32_t vt = st + Block4<D>::offV, vsc = st + Block4<D>::offVS;
+                if constexpr (D == 128) {
+                    const uint4 x = lds128(vt + lane * 16), y = lds128(vt + 512 + lane * 16), z = lds128(vsc + t4 * 32), w = lds128(vsc + t4 * 32 + 16);
+                    va[0][0] = x.x; va[1][0] = x.y; va[0][1] = x.z; va[1][1] = x.w;
+                    va[0][2] = y.x; va[1][2] = y.y; va[0][3] = y.z; va[1][3] = y.w;
+                    vs[0][0] = z.x; vs[0][1] = z.y; vs[1][0] = z.z; vs[1][1] = z.w;
+                    vs[2][0] = w.x; vs[2][1] = w.y; vs[3][0] = w.z; vs[3][1] = w.w;
+                } else {
+                    const uint2 x = lds64(vt + lane * 8), y = lds64(vt + 256 + lane * 8);
+                    const uint4 z = lds128(vsc + t4 * 16);
+                    va[0][0] = x.x; va[0][1] = x.y; va[0][2] = y.x; va[0][3] = y.y;
+                    vs[0][0] = z.x; vs[0][1] = z.y; vs[1][0] = z.z; vs[1][1] = z.w;
+                }
+                if (left < 16) {      // past the end: weights of 0, and whatever the scales there are (they may not be numbers)
+                    const int k = 2 * t4;
+                    const uint32_t m0 = (k < left ? 0xffffu : 0u) | (k + 1 < left ? 0xffff0000u : 0u), m1 = (k + 8 < left ? 0xffffu : 0u) | (k + 9 < left ? 0xffff0000u : 0u);
+#pragma unroll
+                    for (int y = 0; y < kG; ++y) { vs[y][0] &= m0; vs[y][1] &= m1; }
+                }
+#pragma unroll
+                for (int y = 0; y < kG; ++y) {
+                    const uint32_t sel = y % 2 ? 0x7632u : 0x5410u;
+                    const uint32_t w01 = __byte_perm(va[y / 2][0], va[y / 2][1], sel), w23 = __byte_perm(va[y / 2][2], va[y / 2][3], sel);
+                    uint32_t b0[NQ], b1[NQ];
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) { b0[n] = mul2(pb[n][0], vs[y][0]); b1[n] = mul2(pb[n][1], vs[y][1]); }
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        uint32_t v[4];
+                        v[0] = add2(codes128(w01, 2 * u), 0xc308c308u);          // - 136
+                        v[1] = add2(codes128(w01, 2 * u + 1), 0xc308c308u);
+                        v[2] = add2(codes128(w23, 2 * u), 0xc308c308u);
+                        v[3] = add2(codes128(w23, 2 * u + 1), 0xc308c308u);
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) mma16816(o[n][2 * y + u], v, b0[n], b1[n]);
+                    }
+                }
+            } else {
+                const int r = (lane / 16) * 8 + lane % 8;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const int c = 2 * i + (lane / 8 & 1);
+                    uint32_t v[4];
+                    ldmatrix4_trans(v, st + 32 * D + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) mma16816(o[n][i], v, pb[n][0], pb[n][1]);
+                }
+            }
+        }
+        // ---- the segment's end: the warps' results joined, eight queries at a time
+        const bool whole = first == 0 && use.t == use.end;
+        const int slot = 2 * (int)blockIdx.x + (first == 0 ? 1 : 0);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const int rows = min(8, a.G - 8 * n);
+            __syncthreads();                // (the join before has been read)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float lt = l[n][e];
+                lt += __shfl_xor_sync(0xffffffffu, lt, 4);
+                lt += __shfl_xor_sync(0xffffffffu, lt, 8);
+                lt += __shfl_xor_sync(0xffffffffu, lt, 16);
+                const int r = 2 * t4 + e;
+                if (r < rows) {
+                    float *row = merge + (warp * 8 + r) * C::kLd;
+#pragma unroll
+                    for (int i = 0; i < C::kNO; ++i) {
+                        if constexpr (kInt4) {
+                            if (i % 2 == 0) *reinterpret_cast<float4 *>(row + 16 * i + 4 * g) = make_float4(o[n][i][e], o[n][i][2 + e], o[n][i + 1][e], o[n][i + 1][2 + e]);
+                        } else {
+                            row[16 * i + g] = o[n][i][e];
+                            row[16 * i + 8 + g] = o[n][i][2 + e];
+                        }
+                    }
+                    if (g == 0) ml[warp * 8 + r] = make_float2(m[n][e], lt);
+                }
+            }
+            __syncthreads();
+            for (int idx = tid; idx < rows * (D / 4); idx += kThreads) {
+                const int r = idx / (D / 4), c = 4 * (idx % (D / 4));
+                float mt = -INFINITY, ls = 0.f;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) mt = fmaxf(mt, ml[w * 8 + r].x);
+                const float ref = mt == -INFINITY ? 0.f : mt;
+                float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) {
+                    const float2 x = ml[w * 8 + r];
+                    const float f = ex2(x.x - ref);
+                    const float4 v = *reinterpret_cast<const float4 *>(merge + (w * 8 + r) * C::kLd + c);
+                    ls = fmaf(x.y, f, ls);
+                    ot.x = fmaf(v.x, f, ot.x); ot.y = fmaf(v.y, f, ot.y); ot.z = fmaf(v.z, f, ot.z); ot.w = fmaf(v.w, f, ot.w);
+                }
+                if (whole) {
+                    const size_t at = (size_t)head * a.G + 8 * n + r;
+                    const float inv = ls == 0.f ? 0.f : 1.f / ls;
+                    *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
+                    if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + log2f(ls)) * kLn2;
+                } else {
+                    const size_t at = (size_t)slot * a.G + 8 * n + r;
+                    *reinterpret_cast<float4 *>(a.part_o + at * D + c) = ot;
+                    if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(mt, ls);
+                }
+            }
+        }
+        if (!whole && first == 0) {
+            // the head's last unit, and whose share that is in
+            const int last = sh.u0 + done - use.t + use.end - 1;
+            int c = (int)((long long)last * sh.ctas / sh.units);
+            while (first_unit(sh.units, c + 1, sh.ctas) <= last) ++c;
+            told = make_int2(head, c);
+        }
+        if (use.t == use.end) {
+            int b = use.b, h = use.h + 1;
+            if (h == a.Hkv) { h = 0; ++b; }
+            use.set(b, h, 0, b == use.b ? use.len : length(b));
+        }
+    }
+    cp_wait<0>();
+    if (tid == 0) a.info[blockIdx.x] = told;
+}
+
+// Heads that lie in several shares: block (c, query) joins the partial results of the head that begins in share c and goes on, its 128 threads in
+// stripes of D / 4 over the shares.
+template <int D>
+__global__ void __launch_bounds__(128)
+paged_merge_kernel(const int2 *__restrict__ info, const float *__restrict__ part_o, const float *__restrict__ part_ml, __nv_bfloat16 *__restrict__ out,
+                   float *__restrict__ lse, int G)
+{
+    constexpr int kLanes = D / 4, kStripes = 128 / kLanes, kBatch = 8;
+    __shared__ float4 so[kStripes][kLanes];
+    __shared__ float2 sml[kStripes];
+    const int ca = (int)blockIdx.x, g = (int)blockIdx.y;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int2 told = after_wait(info)[ca];
+    const int head = told.x, cb = told.y;
+    if (head < 0) return;
+    part_o = after_wait(part_o);
+    part_ml = after_wait(part_ml);
+    const int stripe = (int)threadIdx.x / kLanes, lane = (int)threadIdx.x % kLanes, c = 4 * lane;
+    float mt = -INFINITY, ls = 0.f;
+    float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = ca + stripe; k0 <= cb; k0 += kStripes * kBatch) {
+        float2 ml[kBatch];
+        float4 v[kBatch];
+        float mn = mt;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int k = k0 + u * kStripes;
+            const size_t at = (size_t)(2 * k + (k == ca ? 1 : 0)) * G + g;
+            const bool there = k <= cb;
+            ml[u] = there ? *reinterpret_cast<const float2 *>(part_ml + at * 2) : make_float2(-INFINITY, 0.f);
+            v[u] = there ? *reinterpret_cast<const float4 *>(part_o + at * D + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, ml[u].x);
+        const float ref = mn == -INFINITY ? 0.f : mn, b = ex2(mt - ref);
+        mt = mn;
+        ls *= b;
+        ot.x *= b; ot.y *= b; ot.z *= b; ot.w *= b;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const float f = ex2(ml[u].x - ref);
+            ls = fmaf(ml[u].y, f, ls);
+            ot.x = fmaf(v[u].x, f, ot.x); ot.y = fmaf(v[u].y, f, ot.y); ot.z = fmaf(v[u].z, f, ot.z); ot.w = fmaf(v[u].w, f, ot.w);
+        }
+    }
+    so[stripe][lane] = ot;
+    if (lane == 0) sml[stripe] = make_float2(mt, ls);
+    __syncthreads();
+    if (stripe == 0) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kStripes; ++k) mx = fmaxf(mx, sml[k].x);
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        ls = 0.f;
+        ot = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < kStripes; ++k) {
+            const float f = ex2(sml[k].x - ref);
+            const float4 v = so[k][lane];
+            ls = fmaf(sml[k].y, f, ls);
+            ot.x = fmaf(v.x, f, ot.x); ot.y = fmaf(v.y, f, ot.y); ot.z = fmaf(v.z, f, ot.z); ot.w = fmaf(v.w, f, ot.w);
+        }
+        const float inv = ls == 0.f ? 0.f : 1.f / ls;
+        *reinterpret_cast<uint2 *>(out + ((size_t)head * G + g) * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
+        if (lse && c == 0) lse[(size_t)head * G + g] = ls == 0.f ? -INFINITY : (mx + log2f(ls)) * kLn2;
+    }
+}
+
+int ctas_for(const PagedProblem &p, int per_sm)
+{
+    // (a unit per CTA at least, at the lengths that the table has room for)
+    const long long units = (long long)p.B * p.pool.Hkv * (((long long)p.max_pages * p.pool.page + kUnitKeys - 1) / kUnitKeys), most = (long long)per_sm * device_info().sms;
+    return (int)(units < most ? units : most);
+}
+
+template <int D, bool kInt4, int NQ>
+cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const int *table, const int *lens, void *out, float *lse, void *ws,
+                   cudaStream_t st)
+{
+    using C = Cfg<D, kInt4, NQ>;
+    const cudaError_t e = allow_smem<paged_decode_kernel<D, kInt4, NQ>>(C::kTotal);
+    if (e != cudaSuccess) return e;
+    const int G = p.H / p.pool.Hkv, ctas = ctas_for(p, C::kCtas), most = 4 * device_info().sms;
+    PagedArgs a{};
+    a.q = (const __nv_bfloat16 *)q; a.pool = (const uint8_t *)pool; a.table = table; a.lens = lens;
+    a.out = (__nv_bfloat16 *)out; a.lse = lse;
+    a.part_o = (float *)ws;
+    a.part_ml = a.part_o + (size_t)2 * most * G * D;
+    a.info = (int2 *)(a.part_ml + (size_t)2 * most * G * 2);
+    a.sq = p.sq;
+    a.table_stride = p.table_stride; a.page_stride = p.pool.page_stride;
+    a.B = p.B; a.Hkv = p.pool.Hkv; a.G = G; a.pages = p.pool.pages; a.page = p.pool.page;
+    a.cap = (int)((long long)p.max_pages * p.pool.page);
+    a.by_page = FastDiv((uint32_t)p.pool.page);
+    a.scale_log2 = p.scale * kLog2e;
+    {
+        LaunchScope scope(MOA_KERNEL_OTHER, st);
+        const cudaError_t le = launch_dependent(paged_decode_kernel<D, kInt4, NQ>, dim3((unsigned)ctas), dim3(kThreads), (size_t)C::kTotal, st, a);
+        if (le != cudaSuccess) return le;
+    }
+    LaunchScope scope(MOA_KERNEL_OTHER, st);
+    return launch_dependent(paged_merge_kernel<D>, dim3((unsigned)ctas, (unsigned)G), dim3(128), (size_t)0, st, (const int2 *)a.info, (const float *)a.part_o,
+                            (const float *)a.part_ml, (__nv_bfloat16 *)out, lse, G);
+}
+
+}  // namespace
+
+size_t paged_decode_workspace_bytes(const PagedProblem &p)
+{
+    const size_t most = (size_t)4 * device_info().sms, G = (size_t)(p.H / p.pool.Hkv);
+    return 2 * most * G * (p.pool.d + 2) * sizeof(float) + most * sizeof(int2);
+}
+
+cudaError_t paged_decode(const PagedProblem &p, const void *q, const void *pool, const int *table, const int *lens, void *out, float *lse,
+                         void *ws, cudaStream_t st)
+{
+    const bool two = p.H / p.pool.Hkv > 8;
+    if (p.pool.d == 64) {
+        if (p.pool.int4) return two ? launch<64, true, 2>(p, q, pool, table, lens, out, lse, ws, st) : launch<64, true, 1>(p, q, pool, table, lens, out, lse, ws, st);
+        return two ? launch<64, false, 2>(p, q, pool, table, lens, out, lse, ws, st) : launch<64, false, 1>(p, q, pool, table, lens, out, lse, ws, st);
+    }
+    if (p.pool.int4) return two ? launch<128, true, 2>(p, q, pool, table, lens, out, lse, ws, st) : launch<128, true, 1>(p, q, pool, table, lens, out, lse, ws, st);
+    return two ? launch<128, false, 2>(p, q, pool, table, lens, out, lse, ws, st) : launch<128, false, 1>(p, q, pool, table, lens, out, lse, ws, st);
+}
+
+}  // namespace moa
