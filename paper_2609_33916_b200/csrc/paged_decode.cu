@@ -6,8 +6,8 @@
 // HBM-bound: 4 d (bf16) or 1.125 d (4 bits) bytes per key and K/V head.  Keys as the rows of the tile: a group of up to eight queries costs
 // one product per 256 elements of the cache, half of what the queries as 16 rows would (groups of 9 to 16: two).  What bounds the 4-bit form beside the
 // bytes is its instructions: an SM has about 400 issue slots in the time HBM takes for 16 keys of a head at d = 128 (2304 bytes).  So
-//   * codes become bf16 by one mask-and-or: 0x4300 | c is 128 + c.  K: the 136 too many are taken off in the products' starting value,
-//     -136 sum(q) of the group; V: by one packed subtraction, exact;
+//   * codes become bf16 by one mask (see `nibbles`).  K: the 8 too many are taken off in the products' starting value, -8 sum(q) of the
+//     group; V: by one packed subtraction, exact;
 //   * K's scale multiplies the products of a group of 32, in fp32; V's is multiplied into the weights (bf16, as the weights of the products are);
 //   * the page's layout (cache_layout.cuh) is the one in which a lane's codes and scales are 16-byte words: no exchange of any kind.
 // A warp streams 16 keys at a time through a ring of its own in shared memory (cp.async; no barrier among warps), with the table entries of
@@ -94,8 +94,18 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Two codes as bf16: 128 + c each (nibbles i and 4 + i of w)
-__device__ __forceinline__ uint32_t codes128(uint32_t w, int i) { return ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u; }
+// The same from a starting value of its own: rows g and g + 8 begin at (c0, c1)
+__device__ __forceinline__ void mma16816_from(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+}
+// Codes as numbers where they lie: a nibble at bits 0..3 or 4..7 of a bf16 whose other bits are zero is c * 2^-133 or c * 2^-129 (the format is
+// linear from 0 to twice its least normal number), so one mask makes a pair of them.  What they meet is larger by 2^64.
+constexpr int kCodeExp0 = -133, kCodeExp1 = -129, kLift = 64;
+__device__ __forceinline__ uint32_t nibbles(uint32_t w, int i) { return w & (i & 1 ? 0x00f000f0u : 0x000f000fu); }      // w: shifted by 8 for i = 2, 3
+__host__ __device__ constexpr float exp2i(int e) { return e < 0 ? 0.5f * exp2i(e + 1) : e > 0 ? 2.f * exp2i(e - 1) : 1.f; }
 __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b)
 {
     uint32_t r;
@@ -281,6 +291,9 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
     for (int i = 0; i < S - 1; ++i) request();
 
     // ---- use
+    // 4 bits: the products of the scores come out lowered, the weights (and their sum l) are raised by 2^kUp
+    constexpr float kUp = kInt4 ? (float)kLift : 0.f;
+    const float scale = a.scale_log2 * (kInt4 ? exp2i(-kCodeExp1 - kLift) : 1.f);
     int done = 0;
     int2 told = make_int2(-1, 0);
     while (done < count) {
@@ -296,11 +309,13 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
 #pragma unroll
                 for (int y = 0; y < kG; ++y) {
                     const uint4 v = row < a.G ? *reinterpret_cast<const uint4 *>(src + 32 * y + 8 * t4) : make_uint4(0u, 0u, 0u, 0u);
-                    qf[n][4 * y] = v.x; qf[n][4 * y + 1] = v.y; qf[n][4 * y + 2] = v.z; qf[n][4 * y + 3] = v.w;
                     float s = ((low_bf16(v.x) + high_bf16(v.x)) + (low_bf16(v.y) + high_bf16(v.y))) + ((low_bf16(v.z) + high_bf16(v.z)) + (low_bf16(v.w) + high_bf16(v.w)));
+                    // (even words meet nibbles 0 and 2, odd ones nibbles 1 and 3, which weigh 16 times as much)
+                    const uint32_t up0 = 0x5f805f80u + (4u << 7) * 0x10001u, up1 = 0x5f805f80u;      // 2^68, 2^64
+                    qf[n][4 * y] = mul2(v.x, up0); qf[n][4 * y + 1] = mul2(v.y, up1); qf[n][4 * y + 2] = mul2(v.z, up0); qf[n][4 * y + 3] = mul2(v.w, up1);
                     s += __shfl_xor_sync(0xffffffffu, s, 1);
                     s += __shfl_xor_sync(0xffffffffu, s, 2);
-                    s *= -136.f;
+                    s *= -8.f * exp2i(kCodeExp1 + kLift);
                     bias[n][y][0] = __shfl_sync(0xffffffffu, s, 8 * t4);
                     bias[n][y][1] = __shfl_sync(0xffffffffu, s, 8 * t4 + 4);
                 }
@@ -346,15 +361,15 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
 #pragma unroll
                 for (int y = 0; y < kG; ++y) {
                     uint32_t lo[4], hi[4];
-                    lo[0] = codes128(k0[y], 0); lo[1] = codes128(k1[y], 0); lo[2] = codes128(k0[y], 1); lo[3] = codes128(k1[y], 1);
-                    hi[0] = codes128(k0[y], 2); hi[1] = codes128(k1[y], 2); hi[2] = codes128(k0[y], 3); hi[3] = codes128(k1[y], 3);
+                    lo[0] = nibbles(k0[y], 0); lo[1] = nibbles(k1[y], 0); lo[2] = nibbles(k0[y], 1); lo[3] = nibbles(k1[y], 1);
+                    hi[0] = nibbles(k0[y] >> 8, 2); hi[1] = nibbles(k1[y] >> 8, 2); hi[2] = nibbles(k0[y] >> 8, 3); hi[3] = nibbles(k1[y] >> 8, 3);
                     // scales: words [row g: groups 0 1, 2 3][row g + 8: 0 1, 2 3]
                     const uint32_t w0 = ks[y / 2], w1 = ks[kG / 2 + y / 2];
                     const float s0 = y % 2 ? high_bf16(w0) : low_bf16(w0), s1 = y % 2 ? high_bf16(w1) : low_bf16(w1);
 #pragma unroll
                     for (int n = 0; n < NQ; ++n) {
-                        float c[4] = {bias[n][y][0], bias[n][y][1], bias[n][y][0], bias[n][y][1]};
-                        mma16816(c, lo, qf[n][4 * y], qf[n][4 * y + 1]);
+                        float c[4];
+                        mma16816_from(c, lo, qf[n][4 * y], qf[n][4 * y + 1], bias[n][y][0], bias[n][y][1]);
                         mma16816(c, hi, qf[n][4 * y + 2], qf[n][4 * y + 3]);
                         sc[n][0] = fmaf(s0, c[0], sc[n][0]);
                         sc[n][1] = fmaf(s0, c[1], sc[n][1]);
@@ -387,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
             for (int n = 0; n < NQ; ++n) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    sc[n][e] *= a.scale_log2;
+                    sc[n][e] *= scale;
                     if (left < 16 && g + 8 * (e / 2) >= left) sc[n][e] = -INFINITY;
                 }
                 grow = grow || fmaxf(sc[n][0], sc[n][2]) > m[n][0] + kRescale || fmaxf(sc[n][1], sc[n][3]) > m[n][1] + kRescale;
@@ -412,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
             uint32_t pb[NQ][2];
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
-                const float r0 = m[n][0] == -INFINITY ? 0.f : m[n][0], r1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
+                const float r0 = (m[n][0] == -INFINITY ? 0.f : m[n][0]) - kUp, r1 = (m[n][1] == -INFINITY ? 0.f : m[n][1]) - kUp;
                 const float p0 = ex2(sc[n][0] - r0), p1 = ex2(sc[n][1] - r1), p2 = ex2(sc[n][2] - r0), p3 = ex2(sc[n][3] - r1);
                 l[n][0] += p0 + p2;
                 l[n][1] += p1 + p3;
@@ -450,10 +465,11 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         uint32_t v[4];
-                        v[0] = add2(codes128(w01, 2 * u), 0xc308c308u);          // - 136
-                        v[1] = add2(codes128(w01, 2 * u + 1), 0xc308c308u);
-                        v[2] = add2(codes128(w23, 2 * u), 0xc308c308u);
-                        v[3] = add2(codes128(w23, 2 * u + 1), 0xc308c308u);
+                        const uint32_t x01 = u ? w01 >> 8 : w01, x23 = u ? w23 >> 8 : w23;
+                        v[0] = add2(nibbles(x01, 0), 0x80088008u);          // - 8
+                        v[1] = add2(nibbles(x01, 1), 0x80808080u);
+                        v[2] = add2(nibbles(x23, 0), 0x80088008u);
+                        v[3] = add2(nibbles(x23, 1), 0x80808080u);
 #pragma unroll
                         for (int n = 0; n < NQ; ++n) mma16816(o[n][2 * y + u], v, b0[n], b1[n]);
                     }
@@ -489,13 +505,16 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
 #pragma unroll
                     for (int i = 0; i < C::kNO; ++i) {
                         if constexpr (kInt4) {
-                            if (i % 2 == 0) *reinterpret_cast<float4 *>(row + 16 * i + 4 * g) = make_float4(o[n][i][e], o[n][i][2 + e], o[n][i + 1][e], o[n][i + 1][2 + e]);
+                            constexpr float k0 = exp2i(-kCodeExp0 - kLift), k1 = exp2i(-kCodeExp1 - kLift);
+                            if (i % 2 == 0)
+                                *reinterpret_cast<float4 *>(row + 16 * i + 4 * g) =
+                                    make_float4(k0 * o[n][i][e], k1 * o[n][i][2 + e], k0 * o[n][i + 1][e], k1 * o[n][i + 1][2 + e]);
                         } else {
                             row[16 * i + g] = o[n][i][e];
                             row[16 * i + 8 + g] = o[n][i][2 + e];
                         }
                     }
-                    if (g == 0) ml[warp * 8 + r] = make_float2(m[n][e], lt);
+                    if (g == 0) ml[warp * 8 + r] = make_float2(m[n][e], lt * exp2i(-(int)kUp));
                 }
             }
             __syncthreads();
