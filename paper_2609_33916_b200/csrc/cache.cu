@@ -4,8 +4,8 @@
 // tokens with all their rows (queries, keys, values), the angles of a token are made once and shared through shared memory, and a row is d / 16
 // lanes with two 16-byte pieces each, several rows in flight per lane.
 //
-// K is rounded to the nearest bf16 of the exact rotation.  In 32 bits the rotation is within 4e-7 (|x1| + |x2|) of it (two roundings of
-// products, the angle's, the factor's); where the two ends of that interval round apart, one element in about 3000, it is made again in 64 bits.
+// K is rounded to the nearest bf16 of the exact rotation.  In 32 bits the rotation is within 4.5 * 2^-24 f (|x1| + |x2|) of it (cosine and sine 1.5, the
+// factor, a product and the sum one each); where the two ends of that interval round apart, one element in about 5000, it is made again in 64 bits.
 // So what a key quantises to does not depend on which arithmetic turned it, and a 4-bit page is a function of the bf16 page's bits.
 //
 // Quantising: 32 neighbours share a scale s = bf16(amax / 7); x / s with one correction by the remainder is exact wherever the quotient is a tie
@@ -20,6 +20,9 @@ using namespace ptx;
 constexpr int kThreads = 256, kTokens = 4, kUnroll = 2;
 using Piece = Chunk<__nv_bfloat16, 8>;
 
+// x / d where x may pass 31 bits
+__device__ __forceinline__ long long divide(long long x, const FastDiv &by) { return x < (1LL << 31) ? (long long)by.div((uint32_t)x) : x / by.d; }
+
 struct AppendArgs {
     const __nv_bfloat16 *q, *k, *v;
     const int *pos;
@@ -30,7 +33,7 @@ struct AppendArgs {
     RopeStride sq, sk, sv, so;
     long long page_stride, keys;     // keys: of the whole pool
     int T, H, Hkv, page, d_rot, tt;
-    FastDiv rows;                    // H + 2 H_kv
+    FastDiv rows, by_page;           // H + 2 H_kv, page
     float factor;
 };
 
@@ -44,14 +47,31 @@ __device__ __forceinline__ float round_bf16(double v)
     return (float)__longlong_as_double(b);
 }
 
-// One element of a rotated pair in 64 bits, rounded to bf16: first: f (x1 cos - x2 sin), else f (x2 cos + x1 sin)
-__device__ __noinline__ float exact_turn(float x1, float x2, int pos, float f, float factor, bool first)
+// A rotated pair, f (x1 cos - x2 sin) and f (x2 cos + x1 sin), in 64 bits and rounded to bf16.  The angle is reduced to a part of a turn as a sum of two
+// doubles (1 / (2 pi) has its second part here), so that positions of millions lose nothing.
+__device__ __noinline__ float2 exact_turn(float x1, float x2, int pos, float f, float factor)
 {
+    const double a = (double)pos * (double)f, h = a * 0x1.45f306dc9c883p-3, l = fma(a, 0x1.45f306dc9c883p-3, -h) + a * -0x1.6b01ec5417056p-57;
     double s, c;
-    sincos((double)pos * (double)f, &s, &c);
+    sincospi(2.0 * ((h - rint(h)) + l), &s, &c);
     c *= (double)factor;
     s *= (double)factor;
-    return round_bf16(first ? (double)x1 * c - (double)x2 * s : (double)x2 * c + (double)x1 * s);
+    return make_float2(round_bf16((double)x1 * c - (double)x2 * s), round_bf16((double)x2 * c + (double)x1 * s));
+}
+
+// Element i of eight, by selects (i is known at run time only)
+__device__ __forceinline__ uint32_t bf16_at(const uint4 &w, int i)
+{
+    const uint32_t v = i < 4 ? (i < 2 ? w.x : w.y) : (i < 6 ? w.z : w.w);
+    return i & 1 ? v >> 16 : v & 0xffffu;
+}
+__device__ __forceinline__ void put_bf16(uint4 &w, int i, uint32_t bits)
+{
+    const uint32_t keep = i & 1 ? 0xffffu : 0xffff0000u, put = i & 1 ? bits << 16 : bits;
+    if (i / 2 == 0) w.x = (w.x & keep) | put;
+    if (i / 2 == 1) w.y = (w.y & keep) | put;
+    if (i / 2 == 2) w.z = (w.z & keep) | put;
+    if (i / 2 == 3) w.w = (w.w & keep) | put;
 }
 
 // Of 16 elements of a lane (the lanes of a pair hold a group): codes of 1..15, four bits each in the order of the elements (the first lowest),
@@ -107,22 +127,13 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendArgs a)
     const int *pos = after_wait(a.pos);
     const float *inv_freq = after_wait(a.inv_freq);
     const long long *slots = after_wait(a.slot);
-    for (int i = tid; i < nt * freqs; i += kThreads) {
-        const int t = i / freqs, f = i - t * freqs;
-        float2 cs = position_angle(pos[t0 + t], inv_freq[f]);
-        cs.x *= a.factor;
-        cs.y *= a.factor;
-        write_angle<8>(angles + t * (freqs / 2), np, f, cs);
-    }
-    __syncthreads();
+    const __nv_bfloat16 *q = after_wait(a.q), *k = after_wait(a.k), *v = after_wait(a.v);
     const int r0 = tid / kLanes, p = tid % kLanes, total = nt * (int)a.rows.d;
     const bool turns = p < np;
     const int c0 = turns && !kPairs ? 8 * p : 16 * p, c1 = turns && !kPairs ? freqs + 8 * p : c0 + 8;      // elements, for q and k; v: 16 p and 16 p + 8
-    const __nv_bfloat16 *q = after_wait(a.q), *k = after_wait(a.k), *v = after_wait(a.v);
-    // (all lanes of a warp make the same rounds: the exchanges below are of whole warps)
-    for (int base = (int)blockIdx.y * kPer * kUnroll; base < total; base += kPer * kUnroll * (int)gridDim.y) {
-        Piece x[kUnroll], y[kUnroll];
-        int tok[kUnroll], head[kUnroll], kind[kUnroll];      // kind 0 q, 1 k, 2 v, -1 none
+    Piece x[kUnroll], y[kUnroll];
+    int tok[kUnroll], head[kUnroll], kind[kUnroll];      // kind 0 q, 1 k, 2 v, -1 none
+    auto load = [&](int base) {
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const int row = base + r0 + u * kPer;
@@ -142,35 +153,70 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendArgs a)
                 y[u].w = *reinterpret_cast<const uint4 *>(src + (kind[u] == 2 ? 16 * p + 8 : c1));
             }
         }
+    };
+    // (all lanes of a warp make the same rounds: the exchanges below are of whole warps)
+    const int step = kPer * kUnroll * (int)gridDim.y;
+    int base = (int)blockIdx.y * kPer * kUnroll;
+    load(base);
+    for (int i = tid; i < nt * freqs; i += kThreads) {
+        const int t = i / freqs, f = i - t * freqs;
+        float2 cs = position_angle(pos[t0 + t], inv_freq[f]);
+        cs.x *= a.factor;
+        cs.y *= a.factor;
+        write_angle<8>(angles + t * (freqs / 2), np, f, cs);
+    }
+    __syncthreads();
+    for (;;) {
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             float fx[8], fy[8];
-            x[u].unpack(fx);
-            y[u].unpack(fy);
             if ((kind[u] == 0 || kind[u] == 1) && turns) {
-                float c[8], s[8], gx[8], gy[8];
+                float c[8], s[8];
+                x[u].unpack(fx);
+                y[u].unpack(fy);
                 read_angles<8>(angles + tok[u] * (freqs / 2), np, p, c, s);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) { gx[i] = fx[i]; gy[i] = fy[i]; }
-                rotate<8, kPairs>(fx, fy, c, s);
                 if (kind[u] == 1) {
-                    const float off = 4e-7f * fabsf(a.factor);
+                    const float off = 2.8e-7f * fabsf(a.factor);
+                    float e[8];
+                    uint32_t doubt = 0;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float x1 = kPairs ? (i < 4 ? gx[2 * i] : gy[2 * i - 8]) : gx[i], x2 = kPairs ? (i < 4 ? gx[2 * i + 1] : gy[2 * i - 7]) : gy[i];
-                        float &y1 = kPairs ? (i < 4 ? fx[2 * i] : fy[2 * i - 8]) : fx[i], &y2 = kPairs ? (i < 4 ? fx[2 * i + 1] : fy[2 * i - 7]) : fy[i];
-                        const float e = off * (fabsf(x1) + fabsf(x2));
-                        const uint32_t lo = pack_bf16(y1 - e, y2 - e), hi = pack_bf16(y1 + e, y2 + e);
-                        if (lo != hi) {
-                            const int at = pos[t0 + tok[u]];
-                            const float f = inv_freq[8 * p + i];
-                            y1 = exact_turn(x1, x2, at, f, a.factor, true);
-                            y2 = exact_turn(x1, x2, at, f, a.factor, false);
+                        const float x1 = kPairs ? (i < 4 ? fx[2 * i] : fy[2 * i - 8]) : fx[i], x2 = kPairs ? (i < 4 ? fx[2 * i + 1] : fy[2 * i - 7]) : fy[i];
+                        e[i] = off * (fabsf(x1) + fabsf(x2));
+                    }
+                    rotate<8, kPairs>(fx, fy, c, s);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float y1 = kPairs ? (i < 4 ? fx[2 * i] : fy[2 * i - 8]) : fx[i], y2 = kPairs ? (i < 4 ? fx[2 * i + 1] : fy[2 * i - 7]) : fy[i];
+                        if (pack_bf16(y1 - e[i], y2 - e[i]) != pack_bf16(y1 + e[i], y2 + e[i])) doubt |= 1u << i;
+                    }
+                    const uint4 xi = x[u].w, yi = y[u].w;
+                    x[u].pack(fx);
+                    y[u].pack(fy);
+                    while (doubt) {
+                        const int i = __ffs((int)doubt) - 1;
+                        doubt &= doubt - 1;
+                        const int at1 = kPairs ? 2 * i & 7 : i, at2 = kPairs ? at1 + 1 : i;
+                        const bool first = !kPairs || i < 4;      // (pairs: in the first piece or in the second)
+                        const uint32_t b1 = bf16_at(first ? xi : yi, at1), b2 = bf16_at(kPairs && first ? xi : yi, at2);
+                        const float2 z = exact_turn(__uint_as_float(b1 << 16), __uint_as_float(b2 << 16), pos[t0 + tok[u]], inv_freq[8 * p + i], a.factor);
+                        const uint32_t z1 = __float_as_uint(z.x) >> 16, z2 = __float_as_uint(z.y) >> 16;
+                        if (kPairs && !first) {
+                            put_bf16(y[u].w, at1, z1);
+                            put_bf16(y[u].w, at2, z2);
+                        } else if (kPairs) {
+                            put_bf16(x[u].w, at1, z1);
+                            put_bf16(x[u].w, at2, z2);
+                        } else {
+                            put_bf16(x[u].w, at1, z1);
+                            put_bf16(y[u].w, at2, z2);
                         }
                     }
+                } else {
+                    rotate<8, kPairs>(fx, fy, c, s);
+                    x[u].pack(fx);
+                    y[u].pack(fy);
                 }
-                x[u].pack(fx);
-                y[u].pack(fy);
             }
             if (kind[u] == 0) {
                 __nv_bfloat16 *dst = a.qo + (long long)(t0 + tok[u]) * a.so.token + head[u] * a.so.head;
@@ -180,7 +226,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendArgs a)
             long long at = -1;
             if (kind[u] > 0) at = slots[t0 + tok[u]];
             const bool there = at >= 0 && at < a.keys;
-            const long long pg = there ? at / a.page : 0;
+            const long long pg = there ? divide(at, a.by_page) : 0;
             const int key = there ? (int)(at - pg * a.page) : 0;
             uint8_t *page = a.pool + pg * a.page_stride;
             if constexpr (!kInt4) {
@@ -236,6 +282,9 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendArgs a)
                 }
             }
         }
+        base += step;
+        if (base >= total) break;
+        load(base);
     }
 }
 
@@ -246,6 +295,7 @@ struct GatherArgs {
     RopeStride sk, sv;
     long long page_stride, keys, rows;     // rows: T * 2 H_kv
     int Hkv, page;
+    FastDiv by_rows, by_page;              // 2 H_kv, page
 };
 
 __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&f)[8])
@@ -260,54 +310,70 @@ __device__ __forceinline__ void store8(float *p, const float (&f)[8])
     reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
 }
 
-// A row of a head is d / 8 lanes with 8 elements each; rows in the order token, K or V, head
+// A row of a head is d / 8 lanes with 8 elements each; rows in the order token, K or V, head; kGatherRows rows of a lane in flight, first all their slots,
+// then all their codes and scales
+constexpr int kGatherRows = 4;
+
 template <typename T, int D, bool kInt4>
 __global__ void __launch_bounds__(kThreads) kv_gather_kernel(const GatherArgs a)
 {
-    constexpr int kLanes = D / 8;
+    constexpr int kLanes = D / 8, kPer = kThreads / kLanes;
     grid_dependency_wait();
     grid_launch_dependents();
     const uint8_t *pool = after_wait(a.pool);
     const long long *slots = after_wait(a.slot);
-    const int c = threadIdx.x % kLanes;
-    const long long step = (long long)gridDim.x * (kThreads / kLanes);
-    for (long long row = (long long)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes; row < a.rows; row += step) {
-        const long long t = row / (2 * a.Hkv);
-        const int rest = (int)(row - t * 2 * a.Hkv), v = rest >= a.Hkv, h = rest - v * a.Hkv;
-        const long long at = slots[t];
-        float f[8];
+    const int c = threadIdx.x % kLanes, y = c / 4, t8 = c % 4;
+    using L = Block4<D>;
+    const long long row0 = (long long)blockIdx.x * (kPer * kGatherRows) + threadIdx.x / kLanes;
+    long long at[kGatherRows], t[kGatherRows];
+    int h[kGatherRows], v[kGatherRows];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = 0.f;
-        if (at >= 0 && at < a.keys) {
-            const long long pg = at / a.page;
-            const int key = (int)(at - pg * a.page), r = key % kBlockKeys;
-            const uint8_t *page = pool + pg * a.page_stride;
-            if constexpr (!kInt4) {
-                Piece x;
-                x.w = *reinterpret_cast<const uint4 *>(page + row16(a.page, D, h, v, key) + 16 * c);
-                x.unpack(f);
-            } else {
-                using L = Block4<D>;
-                const uint8_t *blk = page + block4<D>(a.page, h, key / kBlockKeys);
-                const int y = c / 4, t8 = c % 4;
-                uint32_t code;       // eight nibbles in the order of the elements
-                if (v) {
-                    const int sh = 16 * (y % 2);
-                    const uint32_t lo = *reinterpret_cast<const uint32_t *>(blk + L::v_word(r, 2 * t8, y / 2));
-                    const uint32_t hi = *reinterpret_cast<const uint32_t *>(blk + L::v_word(r, 2 * t8 + 1, y / 2));
-                    code = ((lo >> sh) & 0xffffu) | ((hi >> sh) << 16);
-                } else {
-                    code = *reinterpret_cast<const uint32_t *>(blk + L::k_word(r, t8, y));
-                }
-                const float s = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(blk + (v ? L::v_scale(r, y) : L::k_scale(r, y))) << 16);
+    for (int u = 0; u < kGatherRows; ++u) {
+        const long long row = row0 + u * kPer;
+        t[u] = divide(row, a.by_rows);
+        const int rest = (int)(row - t[u] * (2 * a.Hkv));
+        v[u] = rest >= a.Hkv;
+        h[u] = rest - v[u] * a.Hkv;
+        at[u] = row < a.rows ? slots[t[u]] : -1;
+    }
+    uint4 raw[kGatherRows];        // 16 bytes of a row; 4 bits: one or two words of codes, and the scale
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int n = v ? i : 4 * (i % 2) + i / 2;
-                    f[i] = s * (float)((int)((code >> (4 * n)) & 15u) - 8);
-                }
-            }
+    for (int u = 0; u < kGatherRows; ++u) {
+        raw[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (at[u] < 0 || at[u] >= a.keys) continue;
+        const long long pg = divide(at[u], a.by_page);
+        const int key = (int)(at[u] - pg * a.page), r = key % kBlockKeys;
+        const uint8_t *page = pool + pg * a.page_stride;
+        if constexpr (!kInt4) {
+            raw[u] = *reinterpret_cast<const uint4 *>(page + row16(a.page, D, h[u], v[u], key) + 16 * c);
+        } else {
+            const uint8_t *blk = page + block4<D>(a.page, h[u], key / kBlockKeys);
+            raw[u].x = *reinterpret_cast<const uint32_t *>(blk + (v[u] ? L::v_word(r, 2 * t8, y / 2) : L::k_word(r, t8, y)));
+            if (v[u]) raw[u].y = *reinterpret_cast<const uint32_t *>(blk + L::v_word(r, 2 * t8 + 1, y / 2));
+            raw[u].z = *reinterpret_cast<const uint16_t *>(blk + (v[u] ? L::v_scale(r, y) : L::k_scale(r, y)));
         }
-        T *dst = v ? (T *)a.v + t * a.sv.token + h * a.sv.head : (T *)a.k + t * a.sk.token + h * a.sk.head;
+    }
+#pragma unroll
+    for (int u = 0; u < kGatherRows; ++u) {
+        if (row0 + u * kPer >= a.rows) break;
+        float f[8];
+        if constexpr (!kInt4) {
+            Piece x;
+            x.w = raw[u];
+            x.unpack(f);
+        } else {
+            const int sh = 16 * (y % 2);
+            const uint32_t code = v[u] ? ((raw[u].x >> sh) & 0xffffu) | ((raw[u].y >> sh) << 16) : raw[u].x;
+            const float s = __uint_as_float(raw[u].z << 16);
+            // (the places of a group's elements: in order for V, the even ones and then the odd ones for K)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t n = v[u] ? code >> (4 * i) : code >> (4 * (4 * (i % 2) + i / 2));
+                f[i] = s * (float)((int)(n & 15u) - 8);
+            }
+            // (no such slot: scale 0)
+        }
+        T *dst = v[u] ? (T *)a.v + t[u] * a.sv.token + h[u] * a.sv.head : (T *)a.k + t[u] * a.sk.token + h[u] * a.sk.head;
         store8(dst + 8 * c, f);
     }
 }
@@ -323,8 +389,9 @@ cudaError_t launch_append(const AppendArgs &a, bool pairs, dim3 grid, cudaStream
 template <typename T>
 cudaError_t launch_gather(const GatherArgs &a, int d, int int4, cudaStream_t st)
 {
-    const long long per = kThreads / (d / 8), want = (a.rows + per - 1) / per, most = 32LL * device_info().sms;
-    const dim3 grid((unsigned)(want < most ? want : most));
+    const long long per = kThreads / (d / 8) * kGatherRows, blocks = (a.rows + per - 1) / per;
+    if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+    const dim3 grid((unsigned)blocks);
     LaunchScope scope(MOA_KERNEL_OTHER, st);
     if (d == 64)
         return int4 ? launch_dependent(kv_gather_kernel<T, 64, true>, grid, dim3(kThreads), (size_t)0, st, a)
@@ -346,6 +413,7 @@ cudaError_t kv_append(const AppendProblem &p, const void *q, const void *k, cons
     a.keys = (long long)p.pool.pages * p.pool.page;
     a.T = p.T; a.H = p.H; a.Hkv = p.pool.Hkv; a.page = p.pool.page; a.d_rot = p.d_rot;
     a.rows = FastDiv((uint32_t)(p.H + 2 * p.pool.Hkv));
+    a.by_page = FastDiv((uint32_t)p.pool.page);
     a.factor = p.factor;
     const int per = kThreads / (p.pool.d / 16), sms = device_info().sms;
     a.tt = kTokens;
@@ -368,6 +436,8 @@ cudaError_t kv_gather(const CachePool &pool, int T, int dtype, const void *base,
     a.keys = (long long)pool.pages * pool.page;
     a.rows = 2LL * T * pool.Hkv;
     a.Hkv = pool.Hkv; a.page = pool.page;
+    a.by_rows = FastDiv((uint32_t)(2 * pool.Hkv));
+    a.by_page = FastDiv((uint32_t)pool.page);
     return dtype == MOA_F32 ? launch_gather<float>(a, pool.d, pool.int4, st) : launch_gather<__nv_bfloat16>(a, pool.d, pool.int4, st);
 }
 
