@@ -114,7 +114,7 @@ moa_status moa_gemm(const moa_gemm_desc *desc, const void *A, const void *B, con
  * them is needed: any int32 position).  inv_freq [d_rot/2] fp32 and the factor f hold whatever scaling a long context wants.  The
  * gradient of x is the transposed rotation of the gradient of y, with the same factor: moa_rope_bwd.
  * q, q_out: T tokens x H heads x d; k, k_out: T x H_k x d (H_k = 0: none, NULL); pos [T] int32.  Strides are {token, head} in elements
- * ({0, 0}: contiguous [T,H,d]); each a multiple of 16 bytes and at least d, an output's rows must not overlap.  An output
+ * ({0, 0}: contiguous [T,H,d]); each a multiple of 16 bytes, at least d and at most 2^30, an output's rows must not overlap.  An output
  * may be its own input (same address and strides); other overlaps are not allowed.  T, H >= 1; d a multiple of 8 up to 256;
  * d_rot a multiple of 8, 8 <= d_rot <= d; dtype MOA_BF16 or MOA_F32 (fp32 arithmetic, rounded once).  HBM-bound: every element is read and written once. */
 typedef enum { MOA_ROPE_HALF = 0, MOA_ROPE_PAIRS = 1 } moa_rope_layout;

@@ -33,7 +33,7 @@ struct AppendArgs {
     RopeStride sq, sk, sv, so;
     long long page_stride, keys;     // keys: of the whole pool
     int T, H, Hkv, page, d_rot, tt;
-    FastDiv rows, by_page;           // H + 2 H_kv, page
+    FastDiv by_heads, by_kv, by_page;      // H, H_kv, page
     float factor;
 };
 
@@ -76,11 +76,14 @@ __device__ __forceinline__ void put_bf16(uint4 &w, int i, uint32_t bits)
 
 // Of 16 elements of a lane (the lanes of a pair hold a group): codes of 1..15, four bits each in the order of the elements (the first lowest),
 // and the group's scale.
-__device__ __forceinline__ void quantise16(const float (&x)[16], uint32_t (&code)[2], uint16_t &scale)
+__device__ __forceinline__ void quantise16(const Piece &lo, const Piece &hi, uint32_t (&code)[2], uint16_t &scale)
 {
+    float x[2][8];
+    lo.unpack(x[0]);
+    hi.unpack(x[1]);
     uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);      // (NaN is the largest)
+    for (int i = 0; i < 8; ++i) most = max(most, max(__float_as_uint(x[0][i]) & 0x7fffffffu, __float_as_uint(x[1][i]) & 0x7fffffffu));      // (NaN is the largest)
     most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
     const float amax = __uint_as_float(most);
     float s = __bfloat162float(__float2bfloat16_rn(amax / 7.f));
@@ -94,7 +97,7 @@ __device__ __forceinline__ void quantise16(const float (&x)[16], uint32_t (&code
             uint32_t c = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float v = x[8 * w + i], q0 = v * inv, q1 = fmaf(fmaf(-q0, s, v), inv, q0);
+                const float v = x[w][i], q0 = v * inv, q1 = fmaf(fmaf(-q0, s, v), inv, q0);
                 // adding 1.5 * 2^23 leaves the integer, rounded half to even, in the low bits
                 const int n = (int)(__float_as_uint(q1 + 12582912.f) - 0x4b400000u);
                 c |= (uint32_t)(min(max(n, -7), 7) + 8) << (4 * i);
@@ -116,8 +119,66 @@ __device__ __forceinline__ uint32_t even_then_odd(uint32_t c)
     return e | (o << 16);
 }
 
+// Where the codes and the scale of a lane's 16 elements (group y0, half `half` of it) go
+template <int D>
+__device__ __forceinline__ void write_k4(uint8_t *blk, int r, int y0, int half, const uint32_t (&code)[2], uint16_t scale)
+{
+    using L = Block4<D>;
+    *reinterpret_cast<uint32_t *>(blk + L::k_word(r, 2 * half, y0)) = even_then_odd(code[0]);
+    *reinterpret_cast<uint32_t *>(blk + L::k_word(r, 2 * half + 1, y0)) = even_then_odd(code[1]);
+    if (half == 0) *reinterpret_cast<uint16_t *>(blk + L::k_scale(r, y0)) = scale;
+}
+// V: a word holds four elements of two neighbouring groups: the lanes of those have traded halves of their codes
+template <int D>
+__device__ __forceinline__ void write_v4(uint8_t *blk, int r, int y0, int half, const uint32_t (&code)[2], uint32_t trade, uint16_t scale)
+{
+    using L = Block4<D>;
+    const uint32_t mine = code[y0 % 2 ? 1 : 0], even = y0 % 2 ? trade : mine, odd = y0 % 2 ? mine : trade;
+    const int g = 4 * half + (y0 % 2 ? 2 : 0);
+    *reinterpret_cast<uint32_t *>(blk + L::v_word(r, g, y0 / 2)) = (even & 0xffffu) | (odd << 16);
+    *reinterpret_cast<uint32_t *>(blk + L::v_word(r, g + 1, y0 / 2)) = (even >> 16) | (odd & 0xffff0000u);
+    if (half == 0) *reinterpret_cast<uint16_t *>(blk + L::v_scale(r, y0)) = scale;
+}
+
+// The pieces of a key turned and rounded to the nearest bf16 of the exact result.  pos, f: of this lane's pairs
+template <bool kPairs>
+__device__ __forceinline__ void turn_key(Piece &x, Piece &y, const float (&c)[8], const float (&s)[8], float factor, const int *pos, const float *f)
+{
+    float fx[8], fy[8], e[8];
+    const uint4 xi = x.w, yi = y.w;
+    x.unpack(fx);
+    y.unpack(fy);
+    const float off = 2.8e-7f * fabsf(factor);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x1 = kPairs ? (i < 4 ? fx[2 * i] : fy[2 * i - 8]) : fx[i], x2 = kPairs ? (i < 4 ? fx[2 * i + 1] : fy[2 * i - 7]) : fy[i];
+        e[i] = off * (fabsf(x1) + fabsf(x2));
+    }
+    rotate<8, kPairs>(fx, fy, c, s);
+    uint32_t doubt = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float y1 = kPairs ? (i < 4 ? fx[2 * i] : fy[2 * i - 8]) : fx[i], y2 = kPairs ? (i < 4 ? fx[2 * i + 1] : fy[2 * i - 7]) : fy[i];
+        if (pack_bf16(y1 - e[i], y2 - e[i]) != pack_bf16(y1 + e[i], y2 + e[i])) doubt |= 1u << i;
+    }
+    x.pack(fx);
+    y.pack(fy);
+    while (doubt) {
+        const int i = __ffs((int)doubt) - 1;
+        doubt &= doubt - 1;
+        const int at1 = kPairs ? 2 * i & 7 : i, at2 = kPairs ? at1 + 1 : i;
+        const bool first = !kPairs || i < 4;      // (pairs: in the first piece or in the second)
+        const uint32_t b1 = bf16_at(first ? xi : yi, at1), b2 = bf16_at(kPairs && first ? xi : yi, at2);
+        const float2 z = exact_turn(__uint_as_float(b1 << 16), __uint_as_float(b2 << 16), *pos, f[i], factor);
+        const uint32_t z1 = __float_as_uint(z.x) >> 16, z2 = __float_as_uint(z.y) >> 16;
+        if (first) put_bf16(x.w, at1, z1); else put_bf16(y.w, at1, z1);
+        if (kPairs && first) put_bf16(x.w, at2, z2); else put_bf16(y.w, at2, z2);
+    }
+}
+
+// Blocks of a tile of tokens: gridDim.y == 1: one with all its rows; else the last one keys and values, the others the queries
 template <int D, bool kInt4, bool kPairs>
-__global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendArgs a)
+__global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const AppendArgs a)
 {
     constexpr int kLanes = D / 16, kPer = kThreads / kLanes;
     __shared__ float4 angles[kTokens * D / 4];
@@ -128,36 +189,29 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendArgs a)
     const float *inv_freq = after_wait(a.inv_freq);
     const long long *slots = after_wait(a.slot);
     const __nv_bfloat16 *q = after_wait(a.q), *k = after_wait(a.k), *v = after_wait(a.v);
-    const int r0 = tid / kLanes, p = tid % kLanes, total = nt * (int)a.rows.d;
+    const int r0 = tid / kLanes, p = tid % kLanes;
     const bool turns = p < np;
     const int c0 = turns && !kPairs ? 8 * p : 16 * p, c1 = turns && !kPairs ? freqs + 8 * p : c0 + 8;      // elements, for q and k; v: 16 p and 16 p + 8
+    const int qparts = gridDim.y == 1 ? 1 : (int)gridDim.y - 1, qpart = (int)blockIdx.y;
+    const bool kv = gridDim.y == 1 || qpart == qparts;
+    const int qrows = qpart < qparts ? nt * a.H : 0, kvrows = kv ? nt * a.Hkv : 0;
+    // the first rows are on their way while the angles are made
     Piece x[kUnroll], y[kUnroll];
-    int tok[kUnroll], head[kUnroll], kind[kUnroll];      // kind 0 q, 1 k, 2 v, -1 none
-    auto load = [&](int base) {
+    int tok[kUnroll], head[kUnroll];
+    auto load_q = [&](int row) {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int row = base + r0 + u * kPer;
-            kind[u] = -1;
-            tok[u] = head[u] = 0;
-            x[u].w = y[u].w = make_uint4(0u, 0u, 0u, 0u);
-            if (row < total) {
-                tok[u] = (int)a.rows.div((uint32_t)row);
-                const int h = row - tok[u] * (int)a.rows.d;
-                const long long t = t0 + tok[u];
-                kind[u] = h < a.H ? 0 : h < a.H + a.Hkv ? 1 : 2;
-                head[u] = kind[u] == 0 ? h : kind[u] == 1 ? h - a.H : h - a.H - a.Hkv;
-                const __nv_bfloat16 *src = kind[u] == 0   ? q + t * a.sq.token + head[u] * a.sq.head
-                                           : kind[u] == 1 ? k + t * a.sk.token + head[u] * a.sk.head
-                                                          : v + t * a.sv.token + head[u] * a.sv.head;
-                x[u].w = *reinterpret_cast<const uint4 *>(src + (kind[u] == 2 ? 16 * p : c0));
-                y[u].w = *reinterpret_cast<const uint4 *>(src + (kind[u] == 2 ? 16 * p + 8 : c1));
-            }
+        for (int u = 0; u < kUnroll; ++u, row += kPer) {
+            tok[u] = -1;
+            if (row >= qrows) continue;
+            tok[u] = (int)a.by_heads.div((uint32_t)row);
+            head[u] = row - tok[u] * a.H;
+            const __nv_bfloat16 *src = q + a.sq.at(t0 + tok[u], head[u]);
+            x[u].w = *reinterpret_cast<const uint4 *>(src + c0);
+            y[u].w = *reinterpret_cast<const uint4 *>(src + c1);
         }
     };
-    // (all lanes of a warp make the same rounds: the exchanges below are of whole warps)
-    const int step = kPer * kUnroll * (int)gridDim.y;
-    int base = (int)blockIdx.y * kPer * kUnroll;
-    load(base);
+    int row = qpart * (kPer * kUnroll) + r0;
+    load_q(row);
     for (int i = tid; i < nt * freqs; i += kThreads) {
         const int t = i / freqs, f = i - t * freqs;
         float2 cs = position_angle(pos[t0 + t], inv_freq[f]);
@@ -166,125 +220,84 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendArgs a)
         write_angle<8>(angles + t * (freqs / 2), np, f, cs);
     }
     __syncthreads();
-    for (;;) {
+    while (row < qrows) {
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            float fx[8], fy[8];
-            if ((kind[u] == 0 || kind[u] == 1) && turns) {
-                float c[8], s[8];
+            if (tok[u] < 0) continue;
+            if (turns) {
+                float fx[8], fy[8], c[8], s[8];
                 x[u].unpack(fx);
                 y[u].unpack(fy);
                 read_angles<8>(angles + tok[u] * (freqs / 2), np, p, c, s);
-                if (kind[u] == 1) {
-                    const float off = 2.8e-7f * fabsf(a.factor);
-                    float e[8];
-                    uint32_t doubt = 0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float x1 = kPairs ? (i < 4 ? fx[2 * i] : fy[2 * i - 8]) : fx[i], x2 = kPairs ? (i < 4 ? fx[2 * i + 1] : fy[2 * i - 7]) : fy[i];
-                        e[i] = off * (fabsf(x1) + fabsf(x2));
-                    }
-                    rotate<8, kPairs>(fx, fy, c, s);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float y1 = kPairs ? (i < 4 ? fx[2 * i] : fy[2 * i - 8]) : fx[i], y2 = kPairs ? (i < 4 ? fx[2 * i + 1] : fy[2 * i - 7]) : fy[i];
-                        if (pack_bf16(y1 - e[i], y2 - e[i]) != pack_bf16(y1 + e[i], y2 + e[i])) doubt |= 1u << i;
-                    }
-                    const uint4 xi = x[u].w, yi = y[u].w;
-                    x[u].pack(fx);
-                    y[u].pack(fy);
-                    while (doubt) {
-                        const int i = __ffs((int)doubt) - 1;
-                        doubt &= doubt - 1;
-                        const int at1 = kPairs ? 2 * i & 7 : i, at2 = kPairs ? at1 + 1 : i;
-                        const bool first = !kPairs || i < 4;      // (pairs: in the first piece or in the second)
-                        const uint32_t b1 = bf16_at(first ? xi : yi, at1), b2 = bf16_at(kPairs && first ? xi : yi, at2);
-                        const float2 z = exact_turn(__uint_as_float(b1 << 16), __uint_as_float(b2 << 16), pos[t0 + tok[u]], inv_freq[8 * p + i], a.factor);
-                        const uint32_t z1 = __float_as_uint(z.x) >> 16, z2 = __float_as_uint(z.y) >> 16;
-                        if (kPairs && !first) {
-                            put_bf16(y[u].w, at1, z1);
-                            put_bf16(y[u].w, at2, z2);
-                        } else if (kPairs) {
-                            put_bf16(x[u].w, at1, z1);
-                            put_bf16(x[u].w, at2, z2);
-                        } else {
-                            put_bf16(x[u].w, at1, z1);
-                            put_bf16(y[u].w, at2, z2);
-                        }
-                    }
-                } else {
-                    rotate<8, kPairs>(fx, fy, c, s);
-                    x[u].pack(fx);
-                    y[u].pack(fy);
-                }
+                rotate<8, kPairs>(fx, fy, c, s);
+                x[u].pack(fx);
+                y[u].pack(fy);
             }
-            if (kind[u] == 0) {
-                __nv_bfloat16 *dst = a.qo + (long long)(t0 + tok[u]) * a.so.token + head[u] * a.so.head;
-                *reinterpret_cast<uint4 *>(dst + c0) = x[u].w;
-                *reinterpret_cast<uint4 *>(dst + c1) = y[u].w;
-            }
-            long long at = -1;
-            if (kind[u] > 0) at = slots[t0 + tok[u]];
-            const bool there = at >= 0 && at < a.keys;
-            const long long pg = there ? divide(at, a.by_page) : 0;
-            const int key = there ? (int)(at - pg * a.page) : 0;
-            uint8_t *page = a.pool + pg * a.page_stride;
-            if constexpr (!kInt4) {
-                if (there) {
-                    uint8_t *dst = page + row16(a.page, D, head[u], kind[u] - 1, key);
-                    *reinterpret_cast<uint4 *>(dst + 2 * (kind[u] == 2 ? 16 * p : c0)) = x[u].w;
-                    *reinterpret_cast<uint4 *>(dst + 2 * (kind[u] == 2 ? 16 * p + 8 : c1)) = y[u].w;
-                }
-            } else {
-                if (!__any_sync(0xffffffffu, kind[u] > 0)) continue;
-                // the half layout's lanes hold pieces p and p + d_rot / 16: each gets pieces 2 p and 2 p + 1 from the lanes that have them
-                if (!kPairs && __any_sync(0xffffffffu, kind[u] == 1) && np > 0) {
-                    uint4 got[2];
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        const int piece = 2 * p + w, from = lane - p + (piece < 2 * np ? piece % np : p);
-                        const bool second = piece < 2 * np && piece >= np;
-                        const uint32_t xs[4] = {x[u].w.x, x[u].w.y, x[u].w.z, x[u].w.w}, ys[4] = {y[u].w.x, y[u].w.y, y[u].w.z, y[u].w.w};
-                        uint32_t g[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t gx = __shfl_sync(0xffffffffu, xs[i], from), gy = __shfl_sync(0xffffffffu, ys[i], from);
-                            g[i] = second ? gy : gx;
-                        }
-                        got[w] = make_uint4(g[0], g[1], g[2], g[3]);
-                    }
-                    if (kind[u] == 1 && turns) { x[u].w = got[0]; y[u].w = got[1]; }
-                }
-                x[u].unpack(fx);
-                y[u].unpack(fy);
-                float e[16];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) { e[i] = fx[i]; e[8 + i] = fy[i]; }
-                uint32_t code[2];
-                uint16_t scale;
-                quantise16(e, code, scale);
-                const int y0 = p / 2, half = p % 2, r = key % kBlockKeys;      // group, and which 16 of it
-                uint8_t *blk = page + block4<D>(a.page, head[u], key / kBlockKeys);
-                using L = Block4<D>;
-                // V: a word holds four elements of two neighbouring groups: the lanes of those trade halves of their codes
-                const uint32_t trade = __shfl_xor_sync(0xffffffffu, code[y0 % 2 ? 0 : 1], 2);
-                if (there && kind[u] == 1) {
-                    *reinterpret_cast<uint32_t *>(blk + L::k_word(r, 2 * half, y0)) = even_then_odd(code[0]);
-                    *reinterpret_cast<uint32_t *>(blk + L::k_word(r, 2 * half + 1, y0)) = even_then_odd(code[1]);
-                    if (half == 0) *reinterpret_cast<uint16_t *>(blk + L::k_scale(r, y0)) = scale;
-                }
-                if (there && kind[u] == 2) {
-                    const uint32_t mine = code[y0 % 2 ? 1 : 0], even = y0 % 2 ? trade : mine, odd = y0 % 2 ? mine : trade;
-                    const int g = 4 * half + (y0 % 2 ? 2 : 0);
-                    *reinterpret_cast<uint32_t *>(blk + L::v_word(r, g, y0 / 2)) = (even & 0xffffu) | (odd << 16);
-                    *reinterpret_cast<uint32_t *>(blk + L::v_word(r, g + 1, y0 / 2)) = (even >> 16) | (odd & 0xffff0000u);
-                    if (half == 0) *reinterpret_cast<uint16_t *>(blk + L::v_scale(r, y0)) = scale;
-                }
-            }
+            __nv_bfloat16 *dst = a.qo + a.so.at(t0 + tok[u], head[u]);
+            *reinterpret_cast<uint4 *>(dst + c0) = x[u].w;
+            *reinterpret_cast<uint4 *>(dst + c1) = y[u].w;
         }
-        base += step;
-        if (base >= total) break;
-        load(base);
+        row += qparts * (kPer * kUnroll);
+        load_q(row);
+    }
+    // keys and values: a lane has the pieces of both of a head.  (All lanes of a warp make the same rounds: the exchanges are of whole warps.)
+    for (int base = 0; base < kvrows; base += kPer) {
+        const int r = base + r0;
+        const bool in = r < kvrows;
+        const int t = in ? (int)a.by_kv.div((uint32_t)r) : 0, h = in ? r - t * a.Hkv : 0;
+        const __nv_bfloat16 *ks = k + a.sk.at(t0 + t, h), *vs = v + a.sv.at(t0 + t, h);
+        Piece kx, ky, vx, vy;
+        kx.w = *reinterpret_cast<const uint4 *>(ks + c0);
+        ky.w = *reinterpret_cast<const uint4 *>(ks + c1);
+        vx.w = *reinterpret_cast<const uint4 *>(vs + 16 * p);
+        vy.w = *reinterpret_cast<const uint4 *>(vs + 16 * p + 8);
+        const long long at = slots[t0 + t];
+        const bool there = in && at >= 0 && at < a.keys;
+        const long long pg = there ? divide(at, a.by_page) : 0;
+        const int key = there ? (int)(at - pg * a.page) : 0;
+        uint8_t *page = a.pool + pg * a.page_stride;
+        if (turns) {
+            float c[8], s[8];
+            read_angles<8>(angles + t * (freqs / 2), np, p, c, s);
+            turn_key<kPairs>(kx, ky, c, s, a.factor, pos + t0 + t, inv_freq + 8 * p);
+        }
+        if constexpr (!kInt4) {
+            if (there) {
+                uint8_t *dst = page + row16(a.page, D, h, 0, key), *dv = dst + (long long)a.page * (2 * D);
+                *reinterpret_cast<uint4 *>(dst + 2 * c0) = kx.w;
+                *reinterpret_cast<uint4 *>(dst + 2 * c1) = ky.w;
+                *reinterpret_cast<uint4 *>(dv + 32 * p) = vx.w;
+                *reinterpret_cast<uint4 *>(dv + 32 * p + 16) = vy.w;
+            }
+        } else {
+            // the half layout's lanes hold pieces p and p + d_rot / 16: each gets pieces 2 p and 2 p + 1 from the lanes that have them
+            if (!kPairs && np > 0) {
+                uint4 got[2];
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    const int piece = 2 * p + w;
+                    const bool second = piece >= np && turns;
+                    const int from = lane - p + (turns ? (second ? piece - np : piece) : p);
+                    got[w].x = __shfl_sync(0xffffffffu, kx.w.x, from);
+                    got[w].y = __shfl_sync(0xffffffffu, kx.w.y, from);
+                    got[w].z = __shfl_sync(0xffffffffu, kx.w.z, from);
+                    got[w].w = __shfl_sync(0xffffffffu, kx.w.w, from);
+                    const uint32_t y0 = __shfl_sync(0xffffffffu, ky.w.x, from), y1 = __shfl_sync(0xffffffffu, ky.w.y, from);
+                    const uint32_t y2 = __shfl_sync(0xffffffffu, ky.w.z, from), y3 = __shfl_sync(0xffffffffu, ky.w.w, from);
+                    if (second) got[w] = make_uint4(y0, y1, y2, y3);
+                }
+                if (turns) { kx.w = got[0]; ky.w = got[1]; }
+            }
+            const int y0 = p / 2, half = p % 2, rk = key % kBlockKeys;      // group, and which 16 of it
+            uint8_t *blk = page + block4<D>(a.page, h, key / kBlockKeys);
+            uint32_t code[2];
+            uint16_t scale;
+            quantise16(kx, ky, code, scale);
+            if (there) write_k4<D>(blk, rk, y0, half, code, scale);
+            quantise16(vx, vy, code, scale);
+            const uint32_t trade = __shfl_xor_sync(0xffffffffu, code[y0 % 2 ? 0 : 1], 2);
+            if (there) write_v4<D>(blk, rk, y0, half, code, trade, scale);
+        }
     }
 }
 
@@ -293,9 +306,9 @@ struct GatherArgs {
     const long long *slot;
     void *k, *v;
     RopeStride sk, sv;
-    long long page_stride, keys, rows;     // rows: T * 2 H_kv
-    int Hkv, page;
-    FastDiv by_rows, by_page;              // 2 H_kv, page
+    long long page_stride, keys;           // keys: of the whole pool
+    int T, Hkv, page;
+    FastDiv by_page;
 };
 
 __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&f)[8])
@@ -310,71 +323,62 @@ __device__ __forceinline__ void store8(float *p, const float (&f)[8])
     reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
 }
 
-// A row of a head is d / 8 lanes with 8 elements each; rows in the order token, K or V, head; kGatherRows rows of a lane in flight, first all their slots,
-// then all their codes and scales
-constexpr int kGatherRows = 4;
+// A row of a head is d / 8 lanes with 8 elements each.  A block takes 16 tokens (the codes of 16 neighbouring values share sectors) and kGatherRows
+// of their 2 H_kv rows: first their slots, then all codes and scales of a lane are on their way, then the results.
+constexpr int kGatherRows = 4, kGatherTokens = 16;
 
 template <typename T, int D, bool kInt4>
-__global__ void __launch_bounds__(kThreads) kv_gather_kernel(const GatherArgs a)
+__global__ void __launch_bounds__(kGatherTokens * D / 8) kv_gather_kernel(const GatherArgs a)
 {
-    constexpr int kLanes = D / 8, kPer = kThreads / kLanes;
+    constexpr int kLanes = D / 8;
     grid_dependency_wait();
     grid_launch_dependents();
     const uint8_t *pool = after_wait(a.pool);
     const long long *slots = after_wait(a.slot);
-    const int c = threadIdx.x % kLanes, y = c / 4, t8 = c % 4;
+    const int c = threadIdx.x % kLanes, y = c / 4, t8 = c % 4, t = blockIdx.x * kGatherTokens + threadIdx.x / kLanes, first = blockIdx.y * kGatherRows;
     using L = Block4<D>;
-    const long long row0 = (long long)blockIdx.x * (kPer * kGatherRows) + threadIdx.x / kLanes;
-    long long at[kGatherRows], t[kGatherRows];
-    int h[kGatherRows], v[kGatherRows];
-#pragma unroll
-    for (int u = 0; u < kGatherRows; ++u) {
-        const long long row = row0 + u * kPer;
-        t[u] = divide(row, a.by_rows);
-        const int rest = (int)(row - t[u] * (2 * a.Hkv));
-        v[u] = rest >= a.Hkv;
-        h[u] = rest - v[u] * a.Hkv;
-        at[u] = row < a.rows ? slots[t[u]] : -1;
-    }
+    if (t >= a.T) return;
+    const long long at = slots[t];
+    const bool there = at >= 0 && at < a.keys;
+    const long long pg = there ? divide(at, a.by_page) : 0;
+    const int key = there ? (int)(at - pg * a.page) : 0, r = key % kBlockKeys;
+    const uint8_t *page = pool + pg * a.page_stride;
     uint4 raw[kGatherRows];        // 16 bytes of a row; 4 bits: one or two words of codes, and the scale
 #pragma unroll
     for (int u = 0; u < kGatherRows; ++u) {
         raw[u] = make_uint4(0u, 0u, 0u, 0u);
-        if (at[u] < 0 || at[u] >= a.keys) continue;
-        const long long pg = divide(at[u], a.by_page);
-        const int key = (int)(at[u] - pg * a.page), r = key % kBlockKeys;
-        const uint8_t *page = pool + pg * a.page_stride;
+        const int v = first + u >= a.Hkv, h = first + u - v * a.Hkv;
+        if (!there || h >= a.Hkv) continue;
         if constexpr (!kInt4) {
-            raw[u] = *reinterpret_cast<const uint4 *>(page + row16(a.page, D, h[u], v[u], key) + 16 * c);
+            raw[u] = *reinterpret_cast<const uint4 *>(page + row16(a.page, D, h, v, key) + 16 * c);
         } else {
-            const uint8_t *blk = page + block4<D>(a.page, h[u], key / kBlockKeys);
-            raw[u].x = *reinterpret_cast<const uint32_t *>(blk + (v[u] ? L::v_word(r, 2 * t8, y / 2) : L::k_word(r, t8, y)));
-            if (v[u]) raw[u].y = *reinterpret_cast<const uint32_t *>(blk + L::v_word(r, 2 * t8 + 1, y / 2));
-            raw[u].z = *reinterpret_cast<const uint16_t *>(blk + (v[u] ? L::v_scale(r, y) : L::k_scale(r, y)));
+            const uint8_t *blk = page + block4<D>(a.page, h, key / kBlockKeys);
+            raw[u].x = *reinterpret_cast<const uint32_t *>(blk + (v ? L::v_word(r, 2 * t8, y / 2) : L::k_word(r, t8, y)));
+            if (v) raw[u].y = *reinterpret_cast<const uint32_t *>(blk + L::v_word(r, 2 * t8 + 1, y / 2));
+            raw[u].z = *reinterpret_cast<const uint16_t *>(blk + (v ? L::v_scale(r, y) : L::k_scale(r, y)));
         }
     }
 #pragma unroll
     for (int u = 0; u < kGatherRows; ++u) {
-        if (row0 + u * kPer >= a.rows) break;
+        const int v = first + u >= a.Hkv, h = first + u - v * a.Hkv;
+        if (h >= a.Hkv) break;
         float f[8];
         if constexpr (!kInt4) {
             Piece x;
             x.w = raw[u];
             x.unpack(f);
         } else {
+            // (the places of a group's elements: in order for V, the even ones and then the odd ones for K; no such slot: scale 0)
             const int sh = 16 * (y % 2);
-            const uint32_t code = v[u] ? ((raw[u].x >> sh) & 0xffffu) | ((raw[u].y >> sh) << 16) : raw[u].x;
+            const uint32_t code = v ? ((raw[u].x >> sh) & 0xffffu) | ((raw[u].y >> sh) << 16) : raw[u].x;
             const float s = __uint_as_float(raw[u].z << 16);
-            // (the places of a group's elements: in order for V, the even ones and then the odd ones for K)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const uint32_t n = v[u] ? code >> (4 * i) : code >> (4 * (4 * (i % 2) + i / 2));
+                const uint32_t n = v ? code >> (4 * i) : code >> (4 * (4 * (i % 2) + i / 2));
                 f[i] = s * (float)((int)(n & 15u) - 8);
             }
-            // (no such slot: scale 0)
         }
-        T *dst = v[u] ? (T *)a.v + t[u] * a.sv.token + h[u] * a.sv.head : (T *)a.k + t[u] * a.sk.token + h[u] * a.sk.head;
-        store8(dst + 8 * c, f);
+        store8((v ? (T *)a.v + a.sv.at(t, h) : (T *)a.k + a.sk.at(t, h)) + 8 * c, f);
     }
 }
 
@@ -389,15 +393,13 @@ cudaError_t launch_append(const AppendArgs &a, bool pairs, dim3 grid, cudaStream
 template <typename T>
 cudaError_t launch_gather(const GatherArgs &a, int d, int int4, cudaStream_t st)
 {
-    const long long per = kThreads / (d / 8) * kGatherRows, blocks = (a.rows + per - 1) / per;
-    if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-    const dim3 grid((unsigned)blocks);
+    const dim3 grid((unsigned)((a.T + kGatherTokens - 1) / kGatherTokens), (unsigned)((2 * a.Hkv + kGatherRows - 1) / kGatherRows)), block(kGatherTokens * d / 8);
     LaunchScope scope(MOA_KERNEL_OTHER, st);
     if (d == 64)
-        return int4 ? launch_dependent(kv_gather_kernel<T, 64, true>, grid, dim3(kThreads), (size_t)0, st, a)
-                    : launch_dependent(kv_gather_kernel<T, 64, false>, grid, dim3(kThreads), (size_t)0, st, a);
-    return int4 ? launch_dependent(kv_gather_kernel<T, 128, true>, grid, dim3(kThreads), (size_t)0, st, a)
-                : launch_dependent(kv_gather_kernel<T, 128, false>, grid, dim3(kThreads), (size_t)0, st, a);
+        return int4 ? launch_dependent(kv_gather_kernel<T, 64, true>, grid, block, (size_t)0, st, a)
+                    : launch_dependent(kv_gather_kernel<T, 64, false>, grid, block, (size_t)0, st, a);
+    return int4 ? launch_dependent(kv_gather_kernel<T, 128, true>, grid, block, (size_t)0, st, a)
+                : launch_dependent(kv_gather_kernel<T, 128, false>, grid, block, (size_t)0, st, a);
 }
 
 }  // namespace
@@ -412,16 +414,21 @@ cudaError_t kv_append(const AppendProblem &p, const void *q, const void *k, cons
     a.page_stride = p.pool.page_stride;
     a.keys = (long long)p.pool.pages * p.pool.page;
     a.T = p.T; a.H = p.H; a.Hkv = p.pool.Hkv; a.page = p.pool.page; a.d_rot = p.d_rot;
-    a.rows = FastDiv((uint32_t)(p.H + 2 * p.pool.Hkv));
+    a.by_heads = FastDiv((uint32_t)(p.H > 0 ? p.H : 1));
+    a.by_kv = FastDiv((uint32_t)p.pool.Hkv);
     a.by_page = FastDiv((uint32_t)p.pool.page);
     a.factor = p.factor;
     const int per = kThreads / (p.pool.d / 16), sms = device_info().sms;
     a.tt = kTokens;
     while (a.tt > 1 && (p.T + a.tt - 1) / a.tt < 4 * sms) a.tt /= 2;
     const int blocks = (p.T + a.tt - 1) / a.tt;
-    const long long passes = ((long long)a.tt * (int)a.rows.d + per * kUnroll - 1) / (per * kUnroll);
+    // few tokens: keys and values in a block of their own, the queries in as many more as fill the SMs
     int split = 1;
-    while (split < passes && (long long)blocks * split < 2 * sms) ++split;
+    if (p.H > 0 && blocks < 2 * sms) {
+        const int passes = (int)(((long long)a.tt * p.H + per - 1) / per);
+        split = 2;
+        while (split - 1 < passes && (long long)blocks * split < 2 * sms) ++split;
+    }
     const dim3 grid((unsigned)blocks, (unsigned)split);
     if (p.pool.d == 64) return p.pool.int4 ? launch_append<64, true>(a, p.pairs, grid, st) : launch_append<64, false>(a, p.pairs, grid, st);
     return p.pool.int4 ? launch_append<128, true>(a, p.pairs, grid, st) : launch_append<128, false>(a, p.pairs, grid, st);
@@ -434,9 +441,8 @@ cudaError_t kv_gather(const CachePool &pool, int T, int dtype, const void *base,
     a.pool = (const uint8_t *)base; a.slot = slot; a.k = k; a.v = v; a.sk = sk; a.sv = sv;
     a.page_stride = pool.page_stride;
     a.keys = (long long)pool.pages * pool.page;
-    a.rows = 2LL * T * pool.Hkv;
+    a.T = T;
     a.Hkv = pool.Hkv; a.page = pool.page;
-    a.by_rows = FastDiv((uint32_t)(2 * pool.Hkv));
     a.by_page = FastDiv((uint32_t)pool.page);
     return dtype == MOA_F32 ? launch_gather<float>(a, pool.d, pool.int4, st) : launch_gather<__nv_bfloat16>(a, pool.d, pool.int4, st);
 }

@@ -18,18 +18,19 @@ bool aligned(const void *p, unsigned n) { return (reinterpret_cast<uintptr_t>(p)
 bool finite(float v) { return v == v && v - v == 0.f; }
 
 constexpr int kMostHeads = 1 << 16;
+constexpr int64_t kMostStride = 1 << 30;
 
 // {token, head} strides of T tokens x H heads x d; {0, 0} is [T,H,d].  Multiples of 16 bytes, at least d; an output's rows lie apart.
 bool read_stride(const int64_t (&s)[2], int T, int H, int d, int elem, bool output, RopeStride *out)
 {
     if (s[0] == 0 && s[1] == 0) {
-        *out = RopeStride{(long long)H * d, d};
+        *out = RopeStride{H * d, d};
         return true;
     }
     if (s[0] < d || s[1] < d || s[0] % (16 / elem) != 0 || s[1] % (16 / elem) != 0) return false;
-    if (s[0] > (1LL << 40) || s[1] > (1LL << 40)) return false;
+    if (s[0] > kMostStride || s[1] > kMostStride) return false;
     if (output && T > 1 && H > 1 && s[0] < (H - 1) * s[1] + d && s[1] < (T - 1) * s[0] + d) return false;
-    *out = RopeStride{s[0], s[1]};
+    *out = RopeStride{(int)s[0], (int)s[1]};
     return true;
 }
 

@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             const int row = 8 * n + g;
-            const __nv_bfloat16 *src = q + use.b * a.sq.token + (long long)(use.h * a.G + row) * a.sq.head;
+            const __nv_bfloat16 *src = q + a.sq.at(use.b, use.h * a.G + row);
             if constexpr (kInt4) {
 #pragma unroll
                 for (int y = 0; y < kG; ++y) {

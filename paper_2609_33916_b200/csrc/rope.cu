@@ -62,14 +62,14 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a)
             if (row < total) {
                 tok[u] = (int)a.rows.div((uint32_t)row);
                 const int h = row - tok[u] * (int)a.rows.d;
-                const long long t = t0 + tok[u];
+                const int t = t0 + tok[u];
                 const T *src;
                 if (h < a.H) {
-                    src = q + t * a.sq.token + h * a.sq.head;
-                    dst[u] = (T *)a.qo + t * a.so.token + h * a.so.head;
+                    src = q + a.sq.at(t, h);
+                    dst[u] = (T *)a.qo + a.so.at(t, h);
                 } else {
-                    src = k + t * a.sk.token + (h - a.H) * a.sk.head;
-                    dst[u] = (T *)a.ko + t * a.sko.token + (h - a.H) * a.sko.head;
+                    src = k + a.sk.at(t, h - a.H);
+                    dst[u] = (T *)a.ko + a.sko.at(t, h - a.H);
                 }
                 x[u] = *reinterpret_cast<const Chunk<T, V> *>(src + c0);
                 if (two) y[u] = *reinterpret_cast<const Chunk<T, V> *>(src + c1);

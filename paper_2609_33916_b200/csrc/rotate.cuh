@@ -102,9 +102,10 @@ __device__ __forceinline__ void write_angle(float4 *quads, int np, int freq, flo
     reinterpret_cast<float *>(quads + (V / 4 + i / 4) * np + p)[i % 4] = cs.y;
 }
 
-// rope.cu; strides {token, head} in elements
+// rope.cu; strides {token, head} in elements (32 bits: an offset is two wide multiplications)
 struct RopeStride {
-    long long token, head;
+    int token, head;
+    __host__ __device__ __forceinline__ long long at(int t, int h) const { return (long long)t * token + (long long)h * head; }
 };
 struct RopeProblem {
     int T, H, Hk, d, d_rot, pairs;
