@@ -113,7 +113,7 @@ moa_status check_paged(const moa_paged_decode_desc *d, PagedProblem *p)
     if (d->H % d->cache.H_kv != 0 || (d->table_stride != 0 && d->table_stride < d->max_pages)) return MOA_ERR_INVALID_ARG;
     if (d->dtype != MOA_BF16 && d->dtype != MOA_F32) return MOA_ERR_INVALID_ARG;
     if (!finite(d->scale)) return MOA_ERR_INVALID_ARG;
-    if (d->dtype != MOA_BF16 || d->H / d->cache.H_kv > 16) return MOA_ERR_UNSUPPORTED;
+    if (d->dtype != MOA_BF16 || d->H / d->cache.H_kv > 16 || d->scale > 0x1p60f || d->scale < -0x1p60f) return MOA_ERR_UNSUPPORTED;
     // keys of a row of the table, and units of 64 keys of all rows, are counted in 32 bits
     const long long cap = (long long)d->max_pages * d->cache.page;
     if (cap > (1LL << 30) || (cap + 63) / 64 * d->cache.H_kv > (1LL << 30) / d->B || d->table_stride > (1LL << 40)) return MOA_ERR_UNSUPPORTED;

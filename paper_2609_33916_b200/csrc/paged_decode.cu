@@ -10,10 +10,10 @@
 //     group; V: by one packed subtraction, exact;
 //   * K's scale multiplies the products of a group of 32, in fp32; V's is multiplied into the weights (bf16, as the weights of the products are);
 //   * the page's layout (cache_layout.cuh) is the one in which a lane's codes and scales are 16-byte words: no exchange of any kind.
-// A warp streams 16 keys at a time through a ring of its own in shared memory (cp.async; no barrier among warps), with the table entries of
-// its next 32 steps in a register of each lane, fetched a batch ahead.
+// A warp streams 16 (bf16) or 32 keys at a time through a ring of its own in shared memory (cp.async; no barrier among warps), with the table
+// entries of its next 32 steps in registers of the lanes, fetched a batch ahead.
 //
-// Work split: a unit is 64 keys of a K/V head (16 per warp of a CTA).  All units of all sequences, in the order sequence, head, key, are cut into
+// Work split: a unit is 64 (bf16) or 128 keys of a K/V head, a step of each warp of a CTA.  All units of all sequences, in the order sequence, head, key, are cut into
 // equal shares, one per resident CTA, on the device (the host does not know the lengths): every CTA adds up the lengths and finds its
 // share.  A head that lies in one share is written at once; the others leave partial results (at most two per CTA) and a merge kernel, set up meanwhile,
 // joins them: CTA c tells it which head begins in its share and goes on, and where that ends.
@@ -25,7 +25,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kUnitKeys = 16 * kWarps;
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRescale = 8.f;      // weights may exceed 1 by this power of two before the sums are scaled again
 
@@ -40,14 +40,17 @@ struct PagedArgs {
     long long table_stride, page_stride;
     int B, Hkv, G, pages, page, cap;      // cap: keys that a row of the table has room for
     FastDiv by_page;
-    float scale_log2;
+    float scale_log2;           // > 0; the sign (or 0) is q's factor, a pair of bf16
+    uint32_t sign2;
 };
 
 template <int D, bool kInt4, int NQ>
 struct Cfg {
-    static constexpr int kStage = kInt4 ? Block4<D>::kBytes : 16 * D * 4;
-    static constexpr int kCtas = NQ == 2 ? 2 : kInt4 ? 4 : D == 128 ? 2 : 3;          // resident per SM
-    static constexpr int kStages = kInt4 ? (D == 128 ? (NQ == 2 ? 8 : 4) : 8) : D == 128 ? 3 : 4;
+    static constexpr int kSub = kInt4 ? 2 : 1;                                         // blocks of 16 keys that a warp takes in a step
+    static constexpr int kUnitKeys = 16 * kSub * kWarps;
+    static constexpr int kBlock = kInt4 ? Block4<D>::kBytes : 16 * D * 4, kStage = kSub * kBlock;
+    static constexpr int kCtas = NQ == 2 ? 2 : kInt4 ? (D == 128 ? 3 : 4) : D == 128 ? 2 : 3;          // resident per SM
+    static constexpr int kStages = kInt4 ? (NQ == 2 || D == 64 ? 4 : 3) : D == 128 ? 3 : 4;
     static constexpr int kLd = D + 4;                                                  // floats of a row of the merge
     static constexpr int offMerge = kWarps * kStages * kStage;
     static constexpr int offMl = offMerge + kWarps * 8 * kLd * 4;                      // [warps][8] (maximum, sum)
@@ -121,20 +124,20 @@ __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b)
 __device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-__device__ __forceinline__ int units_of(int len) { return len > 0 ? (len + kUnitKeys - 1) / kUnitKeys : 1; }
+template <int kUnitKeys> __device__ __forceinline__ int units_of(int len) { return len > 0 ? (len + kUnitKeys - 1) / kUnitKeys : 1; }
 __device__ __forceinline__ int first_unit(int units, int c, int ctas) { return (int)((long long)units * c / ctas); }
 
 // The share of CTA c: units [u0, u1) of `units`, and the sequence that holds u0 with the units in front of it
 struct Share {
     int units, ctas, u0, u1, b, before;
 };
-__device__ __forceinline__ Share find_share(const PagedArgs &a, const int *lens, int *scan)
+template <int kUnitKeys> __device__ __forceinline__ Share find_share(const PagedArgs &a, const int *lens, int *scan)
 {
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     Share s;
     int sum = 0, first = 0;
     for (int b = tid; b < a.B; b += kThreads) {
-        const int n = units_of(min(lens[b], a.cap));
+        const int n = units_of<kUnitKeys>(min(lens[b], a.cap));
         if (b == tid) first = n;
         sum += n;
     }
@@ -154,7 +157,7 @@ __device__ __forceinline__ Share find_share(const PagedArgs &a, const int *lens,
     const int row = s.u0 / a.Hkv;      // units of one head: the sequence is the one whose sum passes this (all heads have the same)
     int carry = 0;
     for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-        const int b = b0 + tid, n = b0 == 0 ? first : b < a.B ? units_of(min(lens[b], a.cap)) : 0;
+        const int b = b0 + tid, n = b0 == 0 ? first : b < a.B ? units_of<kUnitKeys>(min(lens[b], a.cap)) : 0;
         int incl = n;
         for (int o = 1; o < 32; o <<= 1) {
             const int x = __shfl_up_sync(0xffffffffu, incl, o);
@@ -181,11 +184,11 @@ __device__ __forceinline__ Share find_share(const PagedArgs &a, const int *lens,
 }
 
 // A place in a share: unit t of head h of sequence b, whose length is len
-struct Place {
+template <int kUnitKeys> struct Place {
     int b, h, t, len, end;      // end: units of a head of the sequence
     __device__ __forceinline__ void set(int seq, int head, int unit, int n)
     {
-        b = seq; h = head; t = unit; len = n; end = units_of(n);
+        b = seq; h = head; t = unit; len = n; end = units_of<kUnitKeys>(n);
     }
 };
 
@@ -193,108 +196,116 @@ template <int D, bool kInt4, int NQ>
 __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_decode_kernel(const PagedArgs a)
 {
     using C = Cfg<D, kInt4, NQ>;
-    constexpr int kG = D / 32, S = C::kStages;
+    constexpr int kG = D / 32, S = C::kStages, kSub = C::kSub, kUnitKeys = C::kUnitKeys;
     extern __shared__ __align__(1024) uint8_t smem[];
     float *merge = reinterpret_cast<float *>(smem + C::offMerge);
     float2 *ml = reinterpret_cast<float2 *>(smem + C::offMl);
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, t4 = lane % 4;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32, g = lane / 4, t4 = lane % 4;
     grid_dependency_wait();
     grid_launch_dependents();
     const int *lens = after_wait(a.lens), *table = after_wait(a.table);
     const uint8_t *pool = after_wait(a.pool);
     const __nv_bfloat16 *q = after_wait(a.q);
-    const Share sh = find_share(a, lens, reinterpret_cast<int *>(smem + C::offScan));
+    const Share sh = find_share<kUnitKeys>(a, lens, reinterpret_cast<int *>(smem + C::offScan));
     auto length = [&](int b) { return b < a.B ? max(0, min(lens[b], a.cap)) : 0; };
-    int count = sh.u1 - sh.u0;
+    const int count = sh.u1 - sh.u0;
     if (count == 0) {
         if (tid == 0) a.info[blockIdx.x] = make_int2(-1, 0);
         return;
     }
-    Place use;
+    Place<kUnitKeys> use;
     {
-        const int len = length(sh.b), end = units_of(len), in = sh.u0 - sh.before;
+        const int len = length(sh.b), end = units_of<kUnitKeys>(len), in = sh.u0 - sh.before;
         use.set(sh.b, in / end, in % end, len);
     }
 
     // ---- requests: S - 1 steps ahead of their use
     const uint32_t ring = smem_u32(smem) + warp * S * C::kStage;
-    Place ask = use;
-    int asked = 0, base = ask.t;      // base: unit of the batch's first entry
-    uint32_t live = 0;                // stages that hold keys
-    // where 16 keys of unit t + lane of head h of sequence b begin (their block, or their row of K), as an offset from the pool; -1: no such page
-    auto entry = [&](int b, int h, int t) -> long long {
-        const int key = (t + lane) * kUnitKeys + 16 * warp;
+    Place<kUnitKeys> ask = use;
+    int left_to_ask = count, base = ask.t;      // base: unit of the batch's first entry
+    uint32_t live = 0;                          // which blocks hold keys: bit kSub * stage + block
+    // where the 16 keys of block s of this warp's step in unit t + lane begin (their block, or their row of K), as an offset from the pool; -1: nowhere
+    auto entry = [&](int b, int h, int t, int s) -> long long {
+        const int key = (t + lane) * kUnitKeys + 16 * (kSub * warp + s);
         if (key >= a.cap || b >= a.B) return -1;
         const int at = (int)a.by_page.div((uint32_t)key), in = key - at * a.page, pg = table[b * a.table_stride + at];
         if ((unsigned)pg >= (unsigned)a.pages) return -1;
         return pg * a.page_stride + (kInt4 ? block4<D>(a.page, h, in / kBlockKeys) : row16(a.page, D, h, 0, in));
     };
-    long long cur = entry(ask.b, ask.h, ask.t), nxt;
-    int nlen;
-    Place np;
+    long long cur[kSub], nxt[kSub];
+    int nlen, nb, nh, nt;
     auto fetch_next = [&] {      // the batch behind the current one
-        np = ask;
-        if (base + 32 < ask.end) {
-            np.t = base + 32;
-            nlen = ask.len;
-        } else {
-            np.t = 0;
-            if (++np.h == a.Hkv) { np.h = 0; ++np.b; }
-            nlen = np.b == ask.b ? ask.len : length(np.b);
+        nb = ask.b; nh = ask.h; nt = base + 32; nlen = ask.len;
+        if (nt >= ask.end) {
+            nt = 0;
+            if (++nh == a.Hkv) { nh = 0; ++nb; nlen = length(nb); }
         }
-        nxt = entry(np.b, np.h, np.t);
+#pragma unroll
+        for (int s = 0; s < kSub; ++s) nxt[s] = entry(nb, nh, nt, s);
     };
+#pragma unroll
+    for (int s = 0; s < kSub; ++s) cur[s] = entry(ask.b, ask.h, ask.t, s);
     fetch_next();
-    auto request = [&] {
-        if (asked < count) {
-            const long long at = __shfl_sync(0xffffffffu, cur, ask.t - base);
-            const int key0 = ask.t * kUnitKeys + 16 * warp, left = ask.len - key0;
-            const uint32_t dst = ring + asked % S * C::kStage;
-            live &= ~(1u << (asked % S));
-            if (at >= 0 && left > 0) {
-                live |= 1u << (asked % S);
-                const uint8_t *src = pool + at;
-                if constexpr (kInt4) {
-                    constexpr int kPieces = C::kStage / 16;
+    auto request = [&](int stage) {
+        live &= ~(((1u << kSub) - 1) << (kSub * stage));
+        if (left_to_ask > 0) {
+            --left_to_ask;
+            const int left = ask.len - (ask.t * kUnitKeys + 16 * kSub * warp);
+            const uint32_t dst = ring + stage * C::kStage;
+            const uint8_t *src[kSub];
+            bool ok[kSub];
 #pragma unroll
-                    for (int i = 0; i < (kPieces + 31) / 32; ++i)
-                        if (i * 32 + 32 <= kPieces || i * 32 + lane < kPieces) cp_async16(dst + 16 * (32 * i + lane), src + 16 * (32 * i + lane), 16);
-                } else {
-                    // rows past the end of the sequence are filled with zeros: whatever they hold, their weight is 0
-                    constexpr int kRow = D / 8, kAt = 32 / kRow;
-                    const int c = lane % kRow;
+            for (int s = 0; s < kSub; ++s) {
+                const long long at = __shfl_sync(0xffffffffu, cur[s], ask.t - base);
+                ok[s] = at >= 0 && left > 16 * s;
+                src[s] = pool + (ok[s] ? at : 0);
+                live |= ok[s] ? 1u << (kSub * stage + s) : 0u;
+            }
+            if constexpr (kInt4) {
+                // (two blocks are 9 D / 32 pieces of 16 bytes for each lane; the lanes of the middle one are of both)
+                constexpr int kPieces = C::kBlock / 16;
+                const uint32_t to = dst + 16 * lane;
 #pragma unroll
-                    for (int i = 0; i < 16 / kAt; ++i) {
-                        const int r = i * kAt + lane / kRow, bytes = r < left ? 16 : 0;
-                        const uint32_t to = dst + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16;
-                        const uint8_t *from = src + (bytes ? r * (2 * D) + c * 16 : 0);
-                        cp_async16(to, from, bytes);
-                        cp_async16(to + 32 * D, from + (long long)a.page * (2 * D), bytes);
-                    }
+                for (int i = 0; i < kSub * kPieces / 32 + (kSub * kPieces % 32 ? 1 : 0); ++i) {
+                    const bool second = 32 * i >= kPieces, mixed = !second && 32 * i + 32 > kPieces;
+                    const bool mine = mixed ? 32 * i + lane >= kPieces : second;
+                    const uint8_t *from = (mine ? src[1] - C::kBlock : src[0]) + 16 * (32 * i + lane);
+                    if ((mine ? ok[1] : ok[0]) && (32 * i + 32 <= kSub * kPieces || 32 * i + lane < kSub * kPieces)) cp_async16(to + 512 * i, from, 16);
+                }
+            } else if (ok[0]) {
+                // rows past the end of the sequence are filled with zeros: whatever they hold, their weight is 0
+                constexpr int kRow = D / 8, kAt = 32 / kRow;
+                const int c = lane % kRow;
+#pragma unroll
+                for (int i = 0; i < 16 / kAt; ++i) {
+                    const int r = i * kAt + lane / kRow, bytes = r < left ? 16 : 0;
+                    const uint32_t to = dst + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16;
+                    const uint8_t *from = src[0] + (bytes ? r * (2 * D) + c * 16 : 0);
+                    cp_async16(to, from, bytes);
+                    cp_async16(to + 32 * D, from + (long long)a.page * (2 * D), bytes);
                 }
             }
-            ++asked;
-            if (++ask.t == ask.end) {
-                ask.set(np.b, np.h, 0, nlen);
-                base = 0;
-                cur = nxt;
-                fetch_next();
-            } else if (ask.t == base + 32) {
-                base += 32;
-                cur = nxt;
+            ++ask.t;
+            const bool over = ask.t == ask.end;
+            if (over || ask.t == base + 32) {
+                if (over) ask.set(nb, nh, 0, nlen);
+                base = ask.t;
+#pragma unroll
+                for (int s = 0; s < kSub; ++s) cur[s] = nxt[s];
                 fetch_next();
             }
         }
         cp_commit();
     };
 #pragma unroll
-    for (int i = 0; i < S - 1; ++i) request();
+    for (int i = 0; i < S - 1; ++i) request(i);
 
     // ---- use
     // 4 bits: the products of the scores come out lowered, the weights (and their sum l) are raised by 2^kUp
     constexpr float kUp = kInt4 ? (float)kLift : 0.f;
-    const float scale = a.scale_log2 * (kInt4 ? exp2i(-kCodeExp1 - kLift) : 1.f);
-    int done = 0;
+    const float scale = a.scale_log2 * (kInt4 ? exp2i(-kCodeExp1 - kLift) : 1.f), margin = kRescale / scale;      // scale > 0: q has its sign
+    const uint32_t sign2 = a.sign2;
+    int done = 0, get = 0;      // get: stage of this step
     int2 told = make_int2(-1, 0);
     while (done < count) {
         const int first = use.t, steps = min(use.end - use.t, count - done), head = use.b * a.Hkv + use.h;
@@ -308,7 +319,8 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
             if constexpr (kInt4) {
 #pragma unroll
                 for (int y = 0; y < kG; ++y) {
-                    const uint4 v = row < a.G ? *reinterpret_cast<const uint4 *>(src + 32 * y + 8 * t4) : make_uint4(0u, 0u, 0u, 0u);
+                    uint4 v = row < a.G ? *reinterpret_cast<const uint4 *>(src + 32 * y + 8 * t4) : make_uint4(0u, 0u, 0u, 0u);
+                    v.x = mul2(v.x, sign2); v.y = mul2(v.y, sign2); v.z = mul2(v.z, sign2); v.w = mul2(v.w, sign2);
                     float s = ((low_bf16(v.x) + high_bf16(v.x)) + (low_bf16(v.y) + high_bf16(v.y))) + ((low_bf16(v.z) + high_bf16(v.z)) + (low_bf16(v.w) + high_bf16(v.w)));
                     // (even words meet nibbles 0 and 2, odd ones nibbles 1 and 3, which weigh 16 times as much)
                     const uint32_t up0 = 0x5f805f80u + (4u << 7) * 0x10001u, up1 = 0x5f805f80u;      // 2^68, 2^64
@@ -321,13 +333,15 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < D / 8; ++i) qf[n][i] = row < a.G ? *reinterpret_cast<const uint32_t *>(src + 8 * i + 2 * t4) : 0u;
+                for (int i = 0; i < D / 8; ++i) qf[n][i] = mul2(row < a.G ? *reinterpret_cast<const uint32_t *>(src + 8 * i + 2 * t4) : 0u, sign2);
             }
         }
-        float o[NQ][C::kNO][4], m[NQ][2], l[NQ][2];
+        // weights are 2^(scale * product - ref); a product above `top` moves ref (and top = -inf: nothing seen yet)
+        float o[NQ][C::kNO][4], ref[NQ][2], top[NQ][2], l[NQ][2];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            m[n][0] = m[n][1] = -INFINITY;
+            ref[n][0] = ref[n][1] = -kUp;
+            top[n][0] = top[n][1] = -INFINITY;
             l[n][0] = l[n][1] = 0.f;
 #pragma unroll
             for (int i = 0; i < C::kNO; ++i)
@@ -337,152 +351,181 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
         for (int step = 0; step < steps; ++step, ++done, ++use.t) {
             cp_wait<S - 2>();
             __syncwarp();
-            request();
-            const int key0 = use.t * kUnitKeys + 16 * warp, left = use.len - key0;
-            if (!((live >> (done % S)) & 1u)) continue;
-            const uint32_t st = ring + done % S * C::kStage;
-            float sc[NQ][4];
-            if constexpr (kInt4) {
-                // rows g and g + 8 of the tile are keys; a lane's words are eight elements of each group
-                uint32_t k0[kG], k1[kG], ks[kG];
-                if constexpr (D == 128) {
-                    const uint4 x = lds128(st + g * 64 + t4 * 16), y = lds128(st + (g + 8) * 64 + t4 * 16), z = lds128(st + Block4<D>::offKS + g * 16);
-                    k0[0] = x.x; k0[1] = x.y; k0[2] = x.z; k0[3] = x.w;
-                    k1[0] = y.x; k1[1] = y.y; k1[2] = y.z; k1[3] = y.w;
-                    ks[0] = z.x; ks[1] = z.y; ks[2] = z.z; ks[3] = z.w;
-                } else {
-                    const uint2 x = lds64(st + g * 32 + t4 * 8), y = lds64(st + (g + 8) * 32 + t4 * 8), z = lds64(st + Block4<D>::offKS + g * 8);
-                    k0[0] = x.x; k0[1] = x.y;
-                    k1[0] = y.x; k1[1] = y.y;
-                    ks[0] = z.x; ks[1] = z.y;
-                }
+            const uint32_t st = ring + get * C::kStage, here = live >> (kSub * get);
+            request(get == 0 ? S - 1 : get - 1);      // (into the stage of the step before)
+            get = get == S - 1 ? 0 : get + 1;
+            if (!(here & ((1u << kSub) - 1))) continue;
+            const int left = use.len - (use.t * kUnitKeys + 16 * kSub * warp);
+            float sc[kSub][NQ][4];
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
-#pragma unroll
-                for (int y = 0; y < kG; ++y) {
-                    uint32_t lo[4], hi[4];
-                    lo[0] = nibbles(k0[y], 0); lo[1] = nibbles(k1[y], 0); lo[2] = nibbles(k0[y], 1); lo[3] = nibbles(k1[y], 1);
-                    hi[0] = nibbles(k0[y] >> 8, 2); hi[1] = nibbles(k1[y] >> 8, 2); hi[2] = nibbles(k0[y] >> 8, 3); hi[3] = nibbles(k1[y] >> 8, 3);
-                    // scales: words [row g: groups 0 1, 2 3][row g + 8: 0 1, 2 3]
-                    const uint32_t w0 = ks[y / 2], w1 = ks[kG / 2 + y / 2];
-                    const float s0 = y % 2 ? high_bf16(w0) : low_bf16(w0), s1 = y % 2 ? high_bf16(w1) : low_bf16(w1);
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) {
-                        float c[4];
-                        mma16816_from(c, lo, qf[n][4 * y], qf[n][4 * y + 1], bias[n][y][0], bias[n][y][1]);
-                        mma16816(c, hi, qf[n][4 * y + 2], qf[n][4 * y + 3]);
-                        sc[n][0] = fmaf(s0, c[0], sc[n][0]);
-                        sc[n][1] = fmaf(s0, c[1], sc[n][1]);
-                        sc[n][2] = fmaf(s1, c[2], sc[n][2]);
-                        sc[n][3] = fmaf(s1, c[3], sc[n][3]);
+            for (int s = 0; s < kSub; ++s) {
+                const uint32_t blk = st + s * C::kBlock;
+                if constexpr (kInt4) {
+                    // rows g and g + 8 of the tile are keys; a lane's words are eight elements of each group
+                    uint32_t k0[kG], k1[kG], ks[kG];
+                    if constexpr (D == 128) {
+                        const uint4 x = lds128(blk + g * 64 + t4 * 16), y = lds128(blk + (g + 8) * 64 + t4 * 16), z = lds128(blk + Block4<D>::offKS + g * 16);
+                        k0[0] = x.x; k0[1] = x.y; k0[2] = x.z; k0[3] = x.w;
+                        k1[0] = y.x; k1[1] = y.y; k1[2] = y.z; k1[3] = y.w;
+                        ks[0] = z.x; ks[1] = z.y; ks[2] = z.z; ks[3] = z.w;
+                    } else {
+                        const uint2 x = lds64(blk + g * 32 + t4 * 8), y = lds64(blk + (g + 8) * 32 + t4 * 8), z = lds64(blk + Block4<D>::offKS + g * 8);
+                        k0[0] = x.x; k0[1] = x.y;
+                        k1[0] = y.x; k1[1] = y.y;
+                        ks[0] = z.x; ks[1] = z.y;
                     }
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) sc[s][n][0] = sc[s][n][1] = sc[s][n][2] = sc[s][n][3] = 0.f;
+#pragma unroll
+                    for (int y = 0; y < kG; ++y) {
+                        const uint32_t h0 = k0[y] >> 8, h1 = k1[y] >> 8;
+                        const uint32_t lo[4] = {nibbles(k0[y], 0), nibbles(k1[y], 0), nibbles(k0[y], 1), nibbles(k1[y], 1)};
+                        const uint32_t hi[4] = {nibbles(h0, 2), nibbles(h1, 2), nibbles(h0, 3), nibbles(h1, 3)};
+                        // scales: words [row g: groups 0 1, 2 3][row g + 8: 0 1, 2 3]
+                        const uint32_t w0 = ks[y / 2], w1 = ks[kG / 2 + y / 2];
+                        const float s0 = y % 2 ? high_bf16(w0) : low_bf16(w0), s1 = y % 2 ? high_bf16(w1) : low_bf16(w1);
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) {
+                            float c[4];
+                            mma16816_from(c, lo, qf[n][4 * y], qf[n][4 * y + 1], bias[n][y][0], bias[n][y][1]);
+                            mma16816(c, hi, qf[n][4 * y + 2], qf[n][4 * y + 3]);
+                            sc[s][n][0] = fmaf(s0, c[0], sc[s][n][0]);
+                            sc[s][n][1] = fmaf(s0, c[1], sc[s][n][1]);
+                            sc[s][n][2] = fmaf(s1, c[2], sc[s][n][2]);
+                            sc[s][n][3] = fmaf(s1, c[3], sc[s][n][3]);
+                        }
+                    }
+                } else {
+                    float odd[NQ][4];
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc[s][n][e] = odd[n][e] = 0.f;
+                    const int r = (lane / 8 & 1) * 8 + lane % 8;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        const int c = 2 * i + lane / 16;
+                        uint32_t ka[4];
+                        ldmatrix4(ka, blk + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16);
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) mma16816(i % 2 ? odd[n] : sc[s][n], ka, qf[n][2 * i], qf[n][2 * i + 1]);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc[s][n][e] += odd[n][e];
                 }
-            } else {
-                float odd[NQ][4];
+            }
+            // keys past the end, and blocks that are not there (their stage holds anything)
+            const bool ragged = left < 16 * kSub || (here & ((1u << kSub) - 1)) != (1u << kSub) - 1;
+            if (ragged) {
 #pragma unroll
-                for (int n = 0; n < NQ; ++n)
+                for (int s = 0; s < kSub; ++s) {
+                    const int in = here >> s & 1 ? left - 16 * s : 0;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[n][e] = odd[n][e] = 0.f;
-                const int r = (lane / 8 & 1) * 8 + lane % 8;
+                    for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const int c = 2 * i + lane / 16;
-                    uint32_t ka[4];
-                    ldmatrix4(ka, st + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16);
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) mma16816(i % 2 ? odd[n] : sc[n], ka, qf[n][2 * i], qf[n][2 * i + 1]);
+                        for (int e = 0; e < 4; ++e)
+                            if (g + 8 * (e / 2) >= in) sc[s][n][e] = -INFINITY;
                 }
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[n][e] += odd[n][e];
             }
             bool grow = false;
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) {
+            for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sc[n][e] *= scale;
-                    if (left < 16 && g + 8 * (e / 2) >= left) sc[n][e] = -INFINITY;
+                for (int e = 0; e < 2; ++e) {
+                    float mx = fmaxf(sc[0][n][e], sc[0][n][2 + e]);
+#pragma unroll
+                    for (int s = 1; s < kSub; ++s) mx = fmaxf(mx, fmaxf(sc[s][n][e], sc[s][n][2 + e]));
+                    grow = grow || mx > top[n][e];
                 }
-                grow = grow || fmaxf(sc[n][0], sc[n][2]) > m[n][0] + kRescale || fmaxf(sc[n][1], sc[n][3]) > m[n][1] + kRescale;
-            }
             if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
                 for (int n = 0; n < NQ; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float mx = fmaxf(sc[n][e], sc[n][2 + e]);
+                        float mx = fmaxf(sc[0][n][e], sc[0][n][2 + e]);
+#pragma unroll
+                        for (int s = 1; s < kSub; ++s) mx = fmaxf(mx, fmaxf(sc[s][n][e], sc[s][n][2 + e]));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                        mx = fmaxf(mx, m[n][e]);
-                        const float f = mx == -INFINITY ? 1.f : ex2(m[n][e] - mx);
-                        m[n][e] = mx;
-                        l[n][e] *= f;
+                        const float to = fmaf(mx, scale, -kUp);
+                        if (mx > -INFINITY && (top[n][e] == -INFINITY || to > ref[n][e])) {
+                            const float f = top[n][e] == -INFINITY ? 1.f : ex2(ref[n][e] - to);      // (nothing seen: the sums are 0)
+                            ref[n][e] = to;
+                            top[n][e] = mx + margin;
+                            l[n][e] *= f;
 #pragma unroll
-                        for (int i = 0; i < C::kNO; ++i) { o[n][i][e] *= f; o[n][i][2 + e] *= f; }
+                            for (int i = 0; i < C::kNO; ++i) { o[n][i][e] *= f; o[n][i][2 + e] *= f; }
+                        }
                     }
             }
-            uint32_t pb[NQ][2];
+            uint32_t pb[kSub][NQ][2];
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                const float r0 = (m[n][0] == -INFINITY ? 0.f : m[n][0]) - kUp, r1 = (m[n][1] == -INFINITY ? 0.f : m[n][1]) - kUp;
-                const float p0 = ex2(sc[n][0] - r0), p1 = ex2(sc[n][1] - r1), p2 = ex2(sc[n][2] - r0), p3 = ex2(sc[n][3] - r1);
-                l[n][0] += p0 + p2;
-                l[n][1] += p1 + p3;
-                pb[n][0] = transpose8(pack_bf16(p0, p1));
-                pb[n][1] = transpose8(pack_bf16(p2, p3));
-            }
-            if constexpr (kInt4) {
-                uint32_t va[D / 64][4], vs[kG][2];      // [h][key 2 t, 2 t + 1, 2 t + 8, 2 t + 9]
-                const uint32_t vt = st + Block4<D>::offV, vsc = st + Block4<D>::offVS;
-                if constexpr (D == 128) {
-                    const uint4 x = lds128(vt + lane * 16), y = lds128(vt + 512 + lane * 16), z = lds128(vsc + t4 * 32), w = lds128(vsc + t4 * 32 + 16);
-                    va[0][0] = x.x; va[1][0] = x.y; va[0][1] = x.z; va[1][1] = x.w;
-                    va[0][2] = y.x; va[1][2] = y.y; va[0][3] = y.z; va[1][3] = y.w;
-                    vs[0][0] = z.x; vs[0][1] = z.y; vs[1][0] = z.z; vs[1][1] = z.w;
-                    vs[2][0] = w.x; vs[2][1] = w.y; vs[3][0] = w.z; vs[3][1] = w.w;
+            for (int s = 0; s < kSub; ++s)
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) {
+                    const float p0 = ex2(fmaf(sc[s][n][0], scale, -ref[n][0])), p1 = ex2(fmaf(sc[s][n][1], scale, -ref[n][1]));
+                    const float p2 = ex2(fmaf(sc[s][n][2], scale, -ref[n][0])), p3 = ex2(fmaf(sc[s][n][3], scale, -ref[n][1]));
+                    l[n][0] += p0 + p2;
+                    l[n][1] += p1 + p3;
+                    pb[s][n][0] = transpose8(pack_bf16(p0, p1));
+                    pb[s][n][1] = transpose8(pack_bf16(p2, p3));
+                }
+#pragma unroll
+            for (int s = 0; s < kSub; ++s) {
+                const uint32_t blk = st + s * C::kBlock;
+                if constexpr (kInt4) {
+                    uint32_t va[D / 64][4], vs[kG][2];      // [h][key 2 t, 2 t + 1, 2 t + 8, 2 t + 9]
+                    const uint32_t vt = blk + Block4<D>::offV, vsc = blk + Block4<D>::offVS;
+                    if constexpr (D == 128) {
+                        const uint4 x = lds128(vt + lane * 16), y = lds128(vt + 512 + lane * 16), z = lds128(vsc + t4 * 32), w = lds128(vsc + t4 * 32 + 16);
+                        va[0][0] = x.x; va[1][0] = x.y; va[0][1] = x.z; va[1][1] = x.w;
+                        va[0][2] = y.x; va[1][2] = y.y; va[0][3] = y.z; va[1][3] = y.w;
+                        vs[0][0] = z.x; vs[0][1] = z.y; vs[1][0] = z.z; vs[1][1] = z.w;
+                        vs[2][0] = w.x; vs[2][1] = w.y; vs[3][0] = w.z; vs[3][1] = w.w;
+                    } else {
+                        const uint2 x = lds64(vt + lane * 8), y = lds64(vt + 256 + lane * 8);
+                        const uint4 z = lds128(vsc + t4 * 16);
+                        va[0][0] = x.x; va[0][1] = x.y; va[0][2] = y.x; va[0][3] = y.y;
+                        vs[0][0] = z.x; vs[0][1] = z.y; vs[1][0] = z.z; vs[1][1] = z.w;
+                    }
+                    if (ragged) {      // past the end: weights of 0, and whatever the scales there are (they may not be numbers)
+                        const int in = here >> s & 1 ? left - 16 * s : 0, k = 2 * t4;
+                        const uint32_t m0 = (k < in ? 0xffffu : 0u) | (k + 1 < in ? 0xffff0000u : 0u), m1 = (k + 8 < in ? 0xffffu : 0u) | (k + 9 < in ? 0xffff0000u : 0u);
+#pragma unroll
+                        for (int y = 0; y < kG; ++y) { vs[y][0] &= m0; vs[y][1] &= m1; }
+                    }
+#pragma unroll
+                    for (int y = 0; y < kG; ++y) {
+                        const uint32_t sel = y % 2 ? 0x7632u : 0x5410u;
+                        const uint32_t w01 = __byte_perm(va[y / 2][0], va[y / 2][1], sel), w23 = __byte_perm(va[y / 2][2], va[y / 2][3], sel);
+                        uint32_t b0[NQ], b1[NQ];
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) { b0[n] = mul2(pb[s][n][0], vs[y][0]); b1[n] = mul2(pb[s][n][1], vs[y][1]); }
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const uint32_t x01 = u ? w01 >> 8 : w01, x23 = u ? w23 >> 8 : w23;
+                            uint32_t v[4];
+                            v[0] = add2(nibbles(x01, 0), 0x80088008u);          // - 8
+                            v[1] = add2(nibbles(x01, 1), 0x80808080u);
+                            v[2] = add2(nibbles(x23, 0), 0x80088008u);
+                            v[3] = add2(nibbles(x23, 1), 0x80808080u);
+#pragma unroll
+                            for (int n = 0; n < NQ; ++n) mma16816(o[n][2 * y + u], v, b0[n], b1[n]);
+                        }
+                    }
                 } else {
-                    const uint2 x = lds64(vt + lane * 8), y = lds64(vt + 256 + lane * 8);
-                    const uint4 z = lds128(vsc + t4 * 16);
-                    va[0][0] = x.x; va[0][1] = x.y; va[0][2] = y.x; va[0][3] = y.y;
-                    vs[0][0] = z.x; vs[0][1] = z.y; vs[1][0] = z.z; vs[1][1] = z.w;
-                }
-                if (left < 16) {      // past the end: weights of 0, and whatever the scales there are (they may not be numbers)
-                    const int k = 2 * t4;
-                    const uint32_t m0 = (k < left ? 0xffffu : 0u) | (k + 1 < left ? 0xffff0000u : 0u), m1 = (k + 8 < left ? 0xffffu : 0u) | (k + 9 < left ? 0xffff0000u : 0u);
+                    const int r = (lane / 16) * 8 + lane % 8;
 #pragma unroll
-                    for (int y = 0; y < kG; ++y) { vs[y][0] &= m0; vs[y][1] &= m1; }
-                }
-#pragma unroll
-                for (int y = 0; y < kG; ++y) {
-                    const uint32_t sel = y % 2 ? 0x7632u : 0x5410u;
-                    const uint32_t w01 = __byte_perm(va[y / 2][0], va[y / 2][1], sel), w23 = __byte_perm(va[y / 2][2], va[y / 2][3], sel);
-                    uint32_t b0[NQ], b1[NQ];
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) { b0[n] = mul2(pb[n][0], vs[y][0]); b1[n] = mul2(pb[n][1], vs[y][1]); }
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
+                    for (int i = 0; i < D / 16; ++i) {
+                        const int c = 2 * i + (lane / 8 & 1);
                         uint32_t v[4];
-                        const uint32_t x01 = u ? w01 >> 8 : w01, x23 = u ? w23 >> 8 : w23;
-                        v[0] = add2(nibbles(x01, 0), 0x80088008u);          // - 8
-                        v[1] = add2(nibbles(x01, 1), 0x80808080u);
-                        v[2] = add2(nibbles(x23, 0), 0x80088008u);
-                        v[3] = add2(nibbles(x23, 1), 0x80808080u);
+                        ldmatrix4_trans(v, blk + 32 * D + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16);
 #pragma unroll
-                        for (int n = 0; n < NQ; ++n) mma16816(o[n][2 * y + u], v, b0[n], b1[n]);
+                        for (int n = 0; n < NQ; ++n) mma16816(o[n][i], v, pb[s][n][0], pb[s][n][1]);
                     }
-                }
-            } else {
-                const int r = (lane / 16) * 8 + lane % 8;
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const int c = 2 * i + (lane / 8 & 1);
-                    uint32_t v[4];
-                    ldmatrix4_trans(v, st + 32 * D + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16);
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) mma16816(o[n][i], v, pb[n][0], pb[n][1]);
                 }
             }
         }
@@ -514,7 +557,7 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
                             row[16 * i + 8 + g] = o[n][i][2 + e];
                         }
                     }
-                    if (g == 0) ml[warp * 8 + r] = make_float2(m[n][e], lt * exp2i(-(int)kUp));
+                    if (g == 0) ml[warp * 8 + r] = make_float2(top[n][e] == -INFINITY ? -INFINITY : ref[n][e] + kUp, lt * exp2i(-(int)kUp));
                 }
             }
             __syncthreads();
@@ -631,10 +674,10 @@ paged_merge_kernel(const int2 *__restrict__ info, const float *__restrict__ part
     }
 }
 
-int ctas_for(const PagedProblem &p, int per_sm)
+int ctas_for(const PagedProblem &p, int per_sm, int unit)
 {
     // (a unit per CTA at least, at the lengths that the table has room for)
-    const long long units = (long long)p.B * p.pool.Hkv * (((long long)p.max_pages * p.pool.page + kUnitKeys - 1) / kUnitKeys), most = (long long)per_sm * device_info().sms;
+    const long long units = (long long)p.B * p.pool.Hkv * (((long long)p.max_pages * p.pool.page + unit - 1) / unit), most = (long long)per_sm * device_info().sms;
     return (int)(units < most ? units : most);
 }
 
@@ -645,7 +688,7 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     using C = Cfg<D, kInt4, NQ>;
     const cudaError_t e = allow_smem<paged_decode_kernel<D, kInt4, NQ>>(C::kTotal);
     if (e != cudaSuccess) return e;
-    const int G = p.H / p.pool.Hkv, ctas = ctas_for(p, C::kCtas), most = 4 * device_info().sms;
+    const int G = p.H / p.pool.Hkv, ctas = ctas_for(p, C::kCtas, C::kUnitKeys), most = 4 * device_info().sms;
     PagedArgs a{};
     a.q = (const __nv_bfloat16 *)q; a.pool = (const uint8_t *)pool; a.table = table; a.lens = lens;
     a.out = (__nv_bfloat16 *)out; a.lse = lse;
@@ -657,7 +700,8 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     a.B = p.B; a.Hkv = p.pool.Hkv; a.G = G; a.pages = p.pool.pages; a.page = p.pool.page;
     a.cap = (int)((long long)p.max_pages * p.pool.page);
     a.by_page = FastDiv((uint32_t)p.pool.page);
-    a.scale_log2 = p.scale * kLog2e;
+    a.scale_log2 = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
+    a.sign2 = p.scale == 0.f ? 0u : p.scale > 0.f ? 0x3f803f80u : 0xbf80bf80u;
     {
         LaunchScope scope(MOA_KERNEL_OTHER, st);
         const cudaError_t le = launch_dependent(paged_decode_kernel<D, kInt4, NQ>, dim3((unsigned)ctas), dim3(kThreads), (size_t)C::kTotal, st, a);

@@ -117,7 +117,7 @@ def test_append_pointers():
 
 @pytest.mark.parametrize("kw,want", [(dict(B=0), 1), (dict(H=0), 1), (dict(H=7), 1), (dict(max_pages=0), 1), (dict(scale=float("inf")), 1), (dict(dtype=4), 1),
                                      (dict(table_stride=3), 1), (dict(table_stride=-4), 1), (dict(q_stride=(100, 128)), 1), (dict(H=34), 2), (dict(dtype=mb.MOA_F32), 2),
-                                     (dict(max_pages=1 << 25), 2), (dict(B=1 << 28), 2)])
+                                     (dict(max_pages=1 << 25), 2), (dict(B=1 << 28), 2), (dict(scale=1e20), 2), (dict(scale=-1e20), 2)])
 def test_paged_decode_refuses(kw, want):
     args = dict(B=2, H=8, max_pages=4, scale=0.1)
     args.update(kw)
