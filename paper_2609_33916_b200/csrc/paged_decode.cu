@@ -10,8 +10,9 @@
 //     group; V: by one packed subtraction, exact;
 //   * K's scale multiplies the products of a group of 32, in fp32; V's is multiplied into the weights (bf16, as the weights of the products are);
 //   * the page's layout (cache_layout.cuh) is the one in which a lane's codes and scales are 16-byte words: no exchange of any kind.
-// A warp streams 16 (bf16) or 32 keys at a time through a ring of its own in shared memory (cp.async; no barrier among warps), with the table
-// entries of its next 32 steps in registers of the lanes, fetched a batch ahead.
+// Loads.  4 bits: a fifth warp asks for the blocks of a unit by bulk copies, a lane for each of its eight blocks, with the table entries of the next four
+// units in its lanes and those behind them on their way; a ring of three units.  bf16: a warp streams its 16 keys at a time through a
+// ring of its own (cp.async with the swizzle that ldmatrix wants; no barrier among warps), the entries of its next 32 steps in its lanes.
 //
 // Work split: a unit is 64 (bf16) or 128 keys of a K/V head, a step of each warp of a CTA.  All units of all sequences, in the order sequence, head, key, are cut into
 // equal shares, one per resident CTA, on the device (the host does not know the lengths): every CTA adds up the lengths and finds its
@@ -25,7 +26,8 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kWarps = 4;            // that compute
+enum : uint32_t { PERR_EMPTY = 0x331, PERR_FULL = 0x332 };
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRescale = 8.f;      // weights may exceed 1 by this power of two before the sums are scaled again
 
@@ -42,20 +44,23 @@ struct PagedArgs {
     FastDiv by_page;
     float scale_log2;           // > 0; the sign (or 0) is q's factor, a pair of bf16
     uint32_t sign2;
+    unsigned int *status;
 };
 
 template <int D, bool kInt4, int NQ>
 struct Cfg {
+    static constexpr int kThreads = 32 * (kWarps + (kInt4 ? 1 : 0));
     static constexpr int kSub = kInt4 ? 2 : 1;                                         // blocks of 16 keys that a warp takes in a step
-    static constexpr int kUnitKeys = 16 * kSub * kWarps;
-    static constexpr int kBlock = kInt4 ? Block4<D>::kBytes : 16 * D * 4, kStage = kSub * kBlock;
-    static constexpr int kCtas = NQ == 2 ? 2 : kInt4 ? (D == 128 ? 3 : 4) : D == 128 ? 2 : 3;          // resident per SM
-    static constexpr int kStages = kInt4 ? (NQ == 2 || D == 64 ? 4 : 3) : D == 128 ? 3 : 4;
+    static constexpr int kBlocks = kSub * kWarps, kUnitKeys = 16 * kBlocks;
+    static constexpr int kBlock = kInt4 ? Block4<D>::kBytes : 16 * D * 4;
+    static constexpr int kCtas = NQ == 2 ? 2 : kInt4 || D == 64 ? 3 : 2;               // resident per SM
+    static constexpr int kStages = kInt4 ? (D == 64 ? 6 : NQ == 2 ? 4 : 3) : D == 128 ? 3 : 4;
     static constexpr int kLd = D + 4;                                                  // floats of a row of the merge
-    static constexpr int offMerge = kWarps * kStages * kStage;
+    static constexpr int offMerge = kStages * kBlocks * kBlock;
     static constexpr int offMl = offMerge + kWarps * 8 * kLd * 4;                      // [warps][8] (maximum, sum)
-    static constexpr int offScan = offMl + kWarps * 8 * 8;
-    static constexpr int kTotal = offScan + 64;
+    static constexpr int offBar = offMl + kWarps * 8 * 8;                              // full, empty [stages], then [stages] words: blocks that hold keys
+    static constexpr int offScan = offBar + kStages * 20 + 4;
+    static constexpr int kTotal = (offScan + 48 + 15) / 16 * 16;
     static constexpr int kNO = D / 16;                                                 // tiles of O^T
 };
 
@@ -131,13 +136,14 @@ __device__ __forceinline__ int first_unit(int units, int c, int ctas) { return (
 struct Share {
     int units, ctas, u0, u1, b, before;
 };
-template <int kUnitKeys> __device__ __forceinline__ Share find_share(const PagedArgs &a, const int *lens, int *scan)
+template <class C> __device__ __forceinline__ Share find_share(const PagedArgs &a, const int *lens, int *scan)
 {
+    constexpr int kThreads = C::kThreads, kAll = kThreads / 32;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     Share s;
     int sum = 0, first = 0;
     for (int b = tid; b < a.B; b += kThreads) {
-        const int n = units_of<kUnitKeys>(min(lens[b], a.cap));
+        const int n = units_of<C::kUnitKeys>(min(lens[b], a.cap));
         if (b == tid) first = n;
         sum += n;
     }
@@ -146,7 +152,7 @@ template <int kUnitKeys> __device__ __forceinline__ Share find_share(const Paged
     __syncthreads();
     sum = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) sum += scan[w];
+    for (int w = 0; w < kAll; ++w) sum += scan[w];
     s.units = sum * a.Hkv;
     s.ctas = min((int)gridDim.x, s.units);
     const int c = blockIdx.x;
@@ -157,7 +163,7 @@ template <int kUnitKeys> __device__ __forceinline__ Share find_share(const Paged
     const int row = s.u0 / a.Hkv;      // units of one head: the sequence is the one whose sum passes this (all heads have the same)
     int carry = 0;
     for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-        const int b = b0 + tid, n = b0 == 0 ? first : b < a.B ? units_of<kUnitKeys>(min(lens[b], a.cap)) : 0;
+        const int b = b0 + tid, n = b0 == 0 ? first : b < a.B ? units_of<C::kUnitKeys>(min(lens[b], a.cap)) : 0;
         int incl = n;
         for (int o = 1; o < 32; o <<= 1) {
             const int x = __shfl_up_sync(0xffffffffu, incl, o);
@@ -168,159 +174,64 @@ template <int kUnitKeys> __device__ __forceinline__ Share find_share(const Paged
         __syncthreads();
         int all = 0;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
+        for (int w = 0; w < kAll; ++w) {
             if (w < warp) incl += scan[w];
             all += scan[w];
         }
         incl += carry;
-        if (incl - n <= row && row < incl) { scan[4] = b; scan[5] = incl - n; }
+        if (incl - n <= row && row < incl) { scan[kAll] = b; scan[kAll + 1] = incl - n; }
         carry += all;
         if (carry > row) break;      // (the same in every thread)
     }
     __syncthreads();
-    s.b = scan[4];
-    s.before = scan[5] * a.Hkv;
+    s.b = scan[kAll];
+    s.before = scan[kAll + 1] * a.Hkv;
     return s;
 }
 
 // A place in a share: unit t of head h of sequence b, whose length is len
-template <int kUnitKeys> struct Place {
+template <class C> struct Place {
     int b, h, t, len, end;      // end: units of a head of the sequence
     __device__ __forceinline__ void set(int seq, int head, int unit, int n)
     {
-        b = seq; h = head; t = unit; len = n; end = units_of<kUnitKeys>(n);
+        b = seq; h = head; t = unit; len = n; end = units_of<C::kUnitKeys>(n);
     }
 };
-
-template <int D, bool kInt4, int NQ>
-__global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_decode_kernel(const PagedArgs a)
+__device__ __forceinline__ int length_of(const PagedArgs &a, const int *lens, int b) { return b < a.B ? max(0, min(lens[b], a.cap)) : 0; }
+// Where block `block` of unit t begins (4 bits: the block, bf16: the row of K), as an offset from the pool; -1: the table has no such page
+template <int D, bool kInt4, class C>
+__device__ __forceinline__ long long block_offset(const PagedArgs &a, const int *table, int b, int h, int t, int block)
 {
-    using C = Cfg<D, kInt4, NQ>;
-    constexpr int kG = D / 32, S = C::kStages, kSub = C::kSub, kUnitKeys = C::kUnitKeys;
-    extern __shared__ __align__(1024) uint8_t smem[];
-    float *merge = reinterpret_cast<float *>(smem + C::offMerge);
-    float2 *ml = reinterpret_cast<float2 *>(smem + C::offMl);
-    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32, g = lane / 4, t4 = lane % 4;
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const int *lens = after_wait(a.lens), *table = after_wait(a.table);
-    const uint8_t *pool = after_wait(a.pool);
-    const __nv_bfloat16 *q = after_wait(a.q);
-    const Share sh = find_share<kUnitKeys>(a, lens, reinterpret_cast<int *>(smem + C::offScan));
-    auto length = [&](int b) { return b < a.B ? max(0, min(lens[b], a.cap)) : 0; };
-    const int count = sh.u1 - sh.u0;
-    if (count == 0) {
-        if (tid == 0) a.info[blockIdx.x] = make_int2(-1, 0);
-        return;
-    }
-    Place<kUnitKeys> use;
+    const int key = t * C::kUnitKeys + 16 * block;
+    if (key >= a.cap || b >= a.B) return -1;
+    const int at = (int)a.by_page.div((uint32_t)key), in = key - at * a.page, pg = table[b * a.table_stride + at];
+    if ((unsigned)pg >= (unsigned)a.pages) return -1;
+    return pg * a.page_stride + (kInt4 ? block4<D>(a.page, h, in / kBlockKeys) : row16(a.page, D, h, 0, in));
+}
+
+// What a warp knows of a head: its queries as B operands (times the scale's sign), and, over the keys it has seen, O^T and the weights' sum.
+// Weights are 2^(scale * product - ref); a product above `top` moves ref (top = -inf: nothing seen yet).  4 bits: products of scores come out
+// lowered, the weights and their sum are raised by 2^kUp.
+template <int D, bool kInt4, int NQ>
+struct HeadState {
+    static constexpr int kG = D / 32, kNO = D / 16, kSub = Cfg<D, kInt4, NQ>::kSub;
+    static constexpr float kUp = kInt4 ? (float)kLift : 0.f;
+    uint32_t qf[NQ][kInt4 ? 4 * kG : D / 8];
+    float bias[NQ][kInt4 ? kG : 1][2];      // 4 bits: the products' starting values
+    float o[NQ][kNO][4], ref[NQ][2], top[NQ][2], l[NQ][2];
+
+    __device__ __forceinline__ void begin(const PagedArgs &a, const __nv_bfloat16 *q, int b, int h, int lane)
     {
-        const int len = length(sh.b), end = units_of<kUnitKeys>(len), in = sh.u0 - sh.before;
-        use.set(sh.b, in / end, in % end, len);
-    }
-
-    // ---- requests: S - 1 steps ahead of their use
-    const uint32_t ring = smem_u32(smem) + warp * S * C::kStage;
-    Place<kUnitKeys> ask = use;
-    int left_to_ask = count, base = ask.t;      // base: unit of the batch's first entry
-    uint32_t live = 0;                          // which blocks hold keys: bit kSub * stage + block
-    // where the 16 keys of block s of this warp's step in unit t + lane begin (their block, or their row of K), as an offset from the pool; -1: nowhere
-    auto entry = [&](int b, int h, int t, int s) -> long long {
-        const int key = (t + lane) * kUnitKeys + 16 * (kSub * warp + s);
-        if (key >= a.cap || b >= a.B) return -1;
-        const int at = (int)a.by_page.div((uint32_t)key), in = key - at * a.page, pg = table[b * a.table_stride + at];
-        if ((unsigned)pg >= (unsigned)a.pages) return -1;
-        return pg * a.page_stride + (kInt4 ? block4<D>(a.page, h, in / kBlockKeys) : row16(a.page, D, h, 0, in));
-    };
-    long long cur[kSub], nxt[kSub];
-    int nlen, nb, nh, nt;
-    auto fetch_next = [&] {      // the batch behind the current one
-        nb = ask.b; nh = ask.h; nt = base + 32; nlen = ask.len;
-        if (nt >= ask.end) {
-            nt = 0;
-            if (++nh == a.Hkv) { nh = 0; ++nb; nlen = length(nb); }
-        }
-#pragma unroll
-        for (int s = 0; s < kSub; ++s) nxt[s] = entry(nb, nh, nt, s);
-    };
-#pragma unroll
-    for (int s = 0; s < kSub; ++s) cur[s] = entry(ask.b, ask.h, ask.t, s);
-    fetch_next();
-    auto request = [&](int stage) {
-        live &= ~(((1u << kSub) - 1) << (kSub * stage));
-        if (left_to_ask > 0) {
-            --left_to_ask;
-            const int left = ask.len - (ask.t * kUnitKeys + 16 * kSub * warp);
-            const uint32_t dst = ring + stage * C::kStage;
-            const uint8_t *src[kSub];
-            bool ok[kSub];
-#pragma unroll
-            for (int s = 0; s < kSub; ++s) {
-                const long long at = __shfl_sync(0xffffffffu, cur[s], ask.t - base);
-                ok[s] = at >= 0 && left > 16 * s;
-                src[s] = pool + (ok[s] ? at : 0);
-                live |= ok[s] ? 1u << (kSub * stage + s) : 0u;
-            }
-            if constexpr (kInt4) {
-                // (two blocks are 9 D / 32 pieces of 16 bytes for each lane; the lanes of the middle one are of both)
-                constexpr int kPieces = C::kBlock / 16;
-                const uint32_t to = dst + 16 * lane;
-#pragma unroll
-                for (int i = 0; i < kSub * kPieces / 32 + (kSub * kPieces % 32 ? 1 : 0); ++i) {
-                    const bool second = 32 * i >= kPieces, mixed = !second && 32 * i + 32 > kPieces;
-                    const bool mine = mixed ? 32 * i + lane >= kPieces : second;
-                    const uint8_t *from = (mine ? src[1] - C::kBlock : src[0]) + 16 * (32 * i + lane);
-                    if ((mine ? ok[1] : ok[0]) && (32 * i + 32 <= kSub * kPieces || 32 * i + lane < kSub * kPieces)) cp_async16(to + 512 * i, from, 16);
-                }
-            } else if (ok[0]) {
-                // rows past the end of the sequence are filled with zeros: whatever they hold, their weight is 0
-                constexpr int kRow = D / 8, kAt = 32 / kRow;
-                const int c = lane % kRow;
-#pragma unroll
-                for (int i = 0; i < 16 / kAt; ++i) {
-                    const int r = i * kAt + lane / kRow, bytes = r < left ? 16 : 0;
-                    const uint32_t to = dst + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16;
-                    const uint8_t *from = src[0] + (bytes ? r * (2 * D) + c * 16 : 0);
-                    cp_async16(to, from, bytes);
-                    cp_async16(to + 32 * D, from + (long long)a.page * (2 * D), bytes);
-                }
-            }
-            ++ask.t;
-            const bool over = ask.t == ask.end;
-            if (over || ask.t == base + 32) {
-                if (over) ask.set(nb, nh, 0, nlen);
-                base = ask.t;
-#pragma unroll
-                for (int s = 0; s < kSub; ++s) cur[s] = nxt[s];
-                fetch_next();
-            }
-        }
-        cp_commit();
-    };
-#pragma unroll
-    for (int i = 0; i < S - 1; ++i) request(i);
-
-    // ---- use
-    // 4 bits: the products of the scores come out lowered, the weights (and their sum l) are raised by 2^kUp
-    constexpr float kUp = kInt4 ? (float)kLift : 0.f;
-    const float scale = a.scale_log2 * (kInt4 ? exp2i(-kCodeExp1 - kLift) : 1.f), margin = kRescale / scale;      // scale > 0: q has its sign
-    const uint32_t sign2 = a.sign2;
-    int done = 0, get = 0;      // get: stage of this step
-    int2 told = make_int2(-1, 0);
-    while (done < count) {
-        const int first = use.t, steps = min(use.end - use.t, count - done), head = use.b * a.Hkv + use.h;
-        // the group's queries: B operands, and 4 bits: the products' starting values
-        uint32_t qf[NQ][kInt4 ? 4 * kG : D / 8];
-        float bias[NQ][kInt4 ? kG : 1][2];
+        const int g = lane / 4, t4 = lane % 4;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             const int row = 8 * n + g;
-            const __nv_bfloat16 *src = q + a.sq.at(use.b, use.h * a.G + row);
+            const __nv_bfloat16 *src = q + a.sq.at(b, h * a.G + row);
             if constexpr (kInt4) {
 #pragma unroll
                 for (int y = 0; y < kG; ++y) {
                     uint4 v = row < a.G ? *reinterpret_cast<const uint4 *>(src + 32 * y + 8 * t4) : make_uint4(0u, 0u, 0u, 0u);
-                    v.x = mul2(v.x, sign2); v.y = mul2(v.y, sign2); v.z = mul2(v.z, sign2); v.w = mul2(v.w, sign2);
+                    v.x = mul2(v.x, a.sign2); v.y = mul2(v.y, a.sign2); v.z = mul2(v.z, a.sign2); v.w = mul2(v.w, a.sign2);
                     float s = ((low_bf16(v.x) + high_bf16(v.x)) + (low_bf16(v.y) + high_bf16(v.y))) + ((low_bf16(v.z) + high_bf16(v.z)) + (low_bf16(v.w) + high_bf16(v.w)));
                     // (even words meet nibbles 0 and 2, odd ones nibbles 1 and 3, which weigh 16 times as much)
                     const uint32_t up0 = 0x5f805f80u + (4u << 7) * 0x10001u, up1 = 0x5f805f80u;      // 2^68, 2^64
@@ -333,261 +244,295 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < D / 8; ++i) qf[n][i] = mul2(row < a.G ? *reinterpret_cast<const uint32_t *>(src + 8 * i + 2 * t4) : 0u, sign2);
+                for (int i = 0; i < D / 8; ++i) qf[n][i] = mul2(row < a.G ? *reinterpret_cast<const uint32_t *>(src + 8 * i + 2 * t4) : 0u, a.sign2);
             }
-        }
-        // weights are 2^(scale * product - ref); a product above `top` moves ref (and top = -inf: nothing seen yet)
-        float o[NQ][C::kNO][4], ref[NQ][2], top[NQ][2], l[NQ][2];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
             ref[n][0] = ref[n][1] = -kUp;
             top[n][0] = top[n][1] = -INFINITY;
             l[n][0] = l[n][1] = 0.f;
 #pragma unroll
-            for (int i = 0; i < C::kNO; ++i)
+            for (int i = 0; i < kNO; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[n][i][e] = 0.f;
         }
-        for (int step = 0; step < steps; ++step, ++done, ++use.t) {
-            cp_wait<S - 2>();
-            __syncwarp();
-            const uint32_t st = ring + get * C::kStage, here = live >> (kSub * get);
-            request(get == 0 ? S - 1 : get - 1);      // (into the stage of the step before)
-            get = get == S - 1 ? 0 : get + 1;
-            if (!(here & ((1u << kSub) - 1))) continue;
-            const int left = use.len - (use.t * kUnitKeys + 16 * kSub * warp);
-            float sc[kSub][NQ][4];
+    }
+
+    // scores of a block of 16 keys: rows g and g + 8 of the tile are keys, columns 2 t4 and 2 t4 + 1 queries
+    __device__ __forceinline__ void scores(float (&sc)[NQ][4], uint32_t blk, int lane) const
+    {
+        const int g = lane / 4, t4 = lane % 4;
+        if constexpr (kInt4) {
+            uint32_t k0[kG], k1[kG], ks[kG];      // a lane's words are eight elements of each group
+            if constexpr (D == 128) {
+                const uint4 x = lds128(blk + g * 64 + t4 * 16), y = lds128(blk + (g + 8) * 64 + t4 * 16), z = lds128(blk + Block4<D>::offKS + g * 16);
+                k0[0] = x.x; k0[1] = x.y; k0[2] = x.z; k0[3] = x.w;
+                k1[0] = y.x; k1[1] = y.y; k1[2] = y.z; k1[3] = y.w;
+                ks[0] = z.x; ks[1] = z.y; ks[2] = z.z; ks[3] = z.w;
+            } else {
+                const uint2 x = lds64(blk + g * 32 + t4 * 8), y = lds64(blk + (g + 8) * 32 + t4 * 8), z = lds64(blk + Block4<D>::offKS + g * 8);
+                k0[0] = x.x; k0[1] = x.y;
+                k1[0] = y.x; k1[1] = y.y;
+                ks[0] = z.x; ks[1] = z.y;
+            }
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
+#pragma unroll
+            for (int y = 0; y < kG; ++y) {
+                const uint32_t h0 = k0[y] >> 8, h1 = k1[y] >> 8;
+                const uint32_t lo[4] = {nibbles(k0[y], 0), nibbles(k1[y], 0), nibbles(k0[y], 1), nibbles(k1[y], 1)};
+                const uint32_t hi[4] = {nibbles(h0, 2), nibbles(h1, 2), nibbles(h0, 3), nibbles(h1, 3)};
+                // scales: words [row g: groups 0 1, 2 3][row g + 8: 0 1, 2 3]
+                const uint32_t w0 = ks[y / 2], w1 = ks[kG / 2 + y / 2];
+                const float s0 = y % 2 ? high_bf16(w0) : low_bf16(w0), s1 = y % 2 ? high_bf16(w1) : low_bf16(w1);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) {
+                    float c[4];
+                    mma16816_from(c, lo, qf[n][4 * y], qf[n][4 * y + 1], bias[n][y][0], bias[n][y][1]);
+                    mma16816(c, hi, qf[n][4 * y + 2], qf[n][4 * y + 3]);
+                    sc[n][0] = fmaf(s0, c[0], sc[n][0]);
+                    sc[n][1] = fmaf(s0, c[1], sc[n][1]);
+                    sc[n][2] = fmaf(s1, c[2], sc[n][2]);
+                    sc[n][3] = fmaf(s1, c[3], sc[n][3]);
+                }
+            }
+        } else {
+            float odd[NQ][4];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[n][e] = odd[n][e] = 0.f;
+            const int r = (lane / 8 & 1) * 8 + lane % 8;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                const int c = 2 * i + lane / 16;
+                uint32_t ka[4];
+                ldmatrix4(ka, blk + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) mma16816(i % 2 ? odd[n] : sc[n], ka, qf[n][2 * i], qf[n][2 * i + 1]);
+            }
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[n][e] += odd[n][e];
+        }
+    }
+
+    // O^T += V^T P^T of a block; keys of it from `in` on do not count (their weights are 0; their scales may not be numbers)
+    __device__ __forceinline__ void values(const uint32_t (&pb)[NQ][2], uint32_t blk, int lane, bool ragged, int in)
+    {
+        const int t4 = lane % 4;
+        if constexpr (kInt4) {
+            uint32_t va[D / 64][4], vs[kG][2];      // [h][key 2 t, 2 t + 1, 2 t + 8, 2 t + 9]
+            const uint32_t vt = blk + Block4<D>::offV, vsc = blk + Block4<D>::offVS;
+            if constexpr (D == 128) {
+                const uint4 x = lds128(vt + lane * 16), y = lds128(vt + 512 + lane * 16), z = lds128(vsc + t4 * 32), w = lds128(vsc + t4 * 32 + 16);
+                va[0][0] = x.x; va[1][0] = x.y; va[0][1] = x.z; va[1][1] = x.w;
+                va[0][2] = y.x; va[1][2] = y.y; va[0][3] = y.z; va[1][3] = y.w;
+                vs[0][0] = z.x; vs[0][1] = z.y; vs[1][0] = z.z; vs[1][1] = z.w;
+                vs[2][0] = w.x; vs[2][1] = w.y; vs[3][0] = w.z; vs[3][1] = w.w;
+            } else {
+                const uint2 x = lds64(vt + lane * 8), y = lds64(vt + 256 + lane * 8);
+                const uint4 z = lds128(vsc + t4 * 16);
+                va[0][0] = x.x; va[0][1] = x.y; va[0][2] = y.x; va[0][3] = y.y;
+                vs[0][0] = z.x; vs[0][1] = z.y; vs[1][0] = z.z; vs[1][1] = z.w;
+            }
+            if (ragged) {
+                const int k = 2 * t4;
+                const uint32_t m0 = (k < in ? 0xffffu : 0u) | (k + 1 < in ? 0xffff0000u : 0u), m1 = (k + 8 < in ? 0xffffu : 0u) | (k + 9 < in ? 0xffff0000u : 0u);
+#pragma unroll
+                for (int y = 0; y < kG; ++y) { vs[y][0] &= m0; vs[y][1] &= m1; }
+            }
+#pragma unroll
+            for (int y = 0; y < kG; ++y) {
+                const uint32_t sel = y % 2 ? 0x7632u : 0x5410u;
+                const uint32_t w01 = __byte_perm(va[y / 2][0], va[y / 2][1], sel), w23 = __byte_perm(va[y / 2][2], va[y / 2][3], sel);
+                uint32_t b0[NQ], b1[NQ];
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) { b0[n] = mul2(pb[n][0], vs[y][0]); b1[n] = mul2(pb[n][1], vs[y][1]); }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t x01 = u ? w01 >> 8 : w01, x23 = u ? w23 >> 8 : w23;
+                    uint32_t v[4];
+                    v[0] = add2(nibbles(x01, 0), 0x80088008u);          // - 8
+                    v[1] = add2(nibbles(x01, 1), 0x80808080u);
+                    v[2] = add2(nibbles(x23, 0), 0x80088008u);
+                    v[3] = add2(nibbles(x23, 1), 0x80808080u);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) mma16816(o[n][2 * y + u], v, b0[n], b1[n]);
+                }
+            }
+        } else {
+            const int r = (lane / 16) * 8 + lane % 8;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                const int c = 2 * i + (lane / 8 & 1);
+                uint32_t v[4];
+                ldmatrix4_trans(v, blk + 32 * D + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) mma16816(o[n][i], v, pb[n][0], pb[n][1]);
+            }
+        }
+    }
+
+    // A step: kSub blocks at `st`; `here`: which of them hold keys (a bit each), `left`: keys of the sequence from the first of them on
+    __device__ __forceinline__ void step(uint32_t st, uint32_t here, int left, float scale, float margin, int lane)
+    {
+        constexpr int kBlock = Cfg<D, kInt4, NQ>::kBlock;
+        constexpr uint32_t kAll = (1u << kSub) - 1;
+        const int g = lane / 4;
+        float sc[kSub][NQ][4];
+#pragma unroll
+        for (int s = 0; s < kSub; ++s) scores(sc[s], st + s * kBlock, lane);
+        // keys past the end, and blocks that are not there (their stage holds anything)
+        const bool ragged = left < 16 * kSub || here != kAll;
+        if (ragged) {
 #pragma unroll
             for (int s = 0; s < kSub; ++s) {
-                const uint32_t blk = st + s * C::kBlock;
-                if constexpr (kInt4) {
-                    // rows g and g + 8 of the tile are keys; a lane's words are eight elements of each group
-                    uint32_t k0[kG], k1[kG], ks[kG];
-                    if constexpr (D == 128) {
-                        const uint4 x = lds128(blk + g * 64 + t4 * 16), y = lds128(blk + (g + 8) * 64 + t4 * 16), z = lds128(blk + Block4<D>::offKS + g * 16);
-                        k0[0] = x.x; k0[1] = x.y; k0[2] = x.z; k0[3] = x.w;
-                        k1[0] = y.x; k1[1] = y.y; k1[2] = y.z; k1[3] = y.w;
-                        ks[0] = z.x; ks[1] = z.y; ks[2] = z.z; ks[3] = z.w;
-                    } else {
-                        const uint2 x = lds64(blk + g * 32 + t4 * 8), y = lds64(blk + (g + 8) * 32 + t4 * 8), z = lds64(blk + Block4<D>::offKS + g * 8);
-                        k0[0] = x.x; k0[1] = x.y;
-                        k1[0] = y.x; k1[1] = y.y;
-                        ks[0] = z.x; ks[1] = z.y;
-                    }
+                const int in = here >> s & 1 ? left - 16 * s : 0;
 #pragma unroll
-                    for (int n = 0; n < NQ; ++n) sc[s][n][0] = sc[s][n][1] = sc[s][n][2] = sc[s][n][3] = 0.f;
+                for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                    for (int y = 0; y < kG; ++y) {
-                        const uint32_t h0 = k0[y] >> 8, h1 = k1[y] >> 8;
-                        const uint32_t lo[4] = {nibbles(k0[y], 0), nibbles(k1[y], 0), nibbles(k0[y], 1), nibbles(k1[y], 1)};
-                        const uint32_t hi[4] = {nibbles(h0, 2), nibbles(h1, 2), nibbles(h0, 3), nibbles(h1, 3)};
-                        // scales: words [row g: groups 0 1, 2 3][row g + 8: 0 1, 2 3]
-                        const uint32_t w0 = ks[y / 2], w1 = ks[kG / 2 + y / 2];
-                        const float s0 = y % 2 ? high_bf16(w0) : low_bf16(w0), s1 = y % 2 ? high_bf16(w1) : low_bf16(w1);
-#pragma unroll
-                        for (int n = 0; n < NQ; ++n) {
-                            float c[4];
-                            mma16816_from(c, lo, qf[n][4 * y], qf[n][4 * y + 1], bias[n][y][0], bias[n][y][1]);
-                            mma16816(c, hi, qf[n][4 * y + 2], qf[n][4 * y + 3]);
-                            sc[s][n][0] = fmaf(s0, c[0], sc[s][n][0]);
-                            sc[s][n][1] = fmaf(s0, c[1], sc[s][n][1]);
-                            sc[s][n][2] = fmaf(s1, c[2], sc[s][n][2]);
-                            sc[s][n][3] = fmaf(s1, c[3], sc[s][n][3]);
-                        }
-                    }
-                } else {
-                    float odd[NQ][4];
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sc[s][n][e] = odd[n][e] = 0.f;
-                    const int r = (lane / 8 & 1) * 8 + lane % 8;
-#pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        const int c = 2 * i + lane / 16;
-                        uint32_t ka[4];
-                        ldmatrix4(ka, blk + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16);
-#pragma unroll
-                        for (int n = 0; n < NQ; ++n) mma16816(i % 2 ? odd[n] : sc[s][n], ka, qf[n][2 * i], qf[n][2 * i + 1]);
-                    }
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sc[s][n][e] += odd[n][e];
-                }
+                    for (int e = 0; e < 4; ++e)
+                        if (g + 8 * (e / 2) >= in) sc[s][n][e] = -INFINITY;
             }
-            // keys past the end, and blocks that are not there (their stage holds anything)
-            const bool ragged = left < 16 * kSub || (here & ((1u << kSub) - 1)) != (1u << kSub) - 1;
-            if (ragged) {
+        }
+        bool grow = false;
+        float mx[NQ][2];
 #pragma unroll
-                for (int s = 0; s < kSub; ++s) {
-                    const int in = here >> s & 1 ? left - 16 * s : 0;
+        for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                    for (int n = 0; n < NQ; ++n)
+            for (int e = 0; e < 2; ++e) {
+                mx[n][e] = fmaxf(sc[0][n][e], sc[0][n][2 + e]);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (g + 8 * (e / 2) >= in) sc[s][n][e] = -INFINITY;
-                }
+                for (int s = 1; s < kSub; ++s) mx[n][e] = fmaxf(mx[n][e], fmaxf(sc[s][n][e], sc[s][n][2 + e]));
+                grow = grow || mx[n][e] > top[n][e];
             }
-            bool grow = false;
+        if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float mx = fmaxf(sc[0][n][e], sc[0][n][2 + e]);
+                    float m = mx[n][e];
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                    const float to = fmaf(m, scale, -kUp);
+                    if (m > -INFINITY && (top[n][e] == -INFINITY || to > ref[n][e])) {
+                        const float f = top[n][e] == -INFINITY ? 1.f : ex2(ref[n][e] - to);      // (nothing seen: the sums are 0)
+                        ref[n][e] = to;
+                        top[n][e] = m + margin;
+                        l[n][e] *= f;
 #pragma unroll
-                    for (int s = 1; s < kSub; ++s) mx = fmaxf(mx, fmaxf(sc[s][n][e], sc[s][n][2 + e]));
-                    grow = grow || mx > top[n][e];
-                }
-            if (__any_sync(0xffffffffu, grow)) {
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float mx = fmaxf(sc[0][n][e], sc[0][n][2 + e]);
-#pragma unroll
-                        for (int s = 1; s < kSub; ++s) mx = fmaxf(mx, fmaxf(sc[s][n][e], sc[s][n][2 + e]));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                        const float to = fmaf(mx, scale, -kUp);
-                        if (mx > -INFINITY && (top[n][e] == -INFINITY || to > ref[n][e])) {
-                            const float f = top[n][e] == -INFINITY ? 1.f : ex2(ref[n][e] - to);      // (nothing seen: the sums are 0)
-                            ref[n][e] = to;
-                            top[n][e] = mx + margin;
-                            l[n][e] *= f;
-#pragma unroll
-                            for (int i = 0; i < C::kNO; ++i) { o[n][i][e] *= f; o[n][i][2 + e] *= f; }
-                        }
+                        for (int i = 0; i < kNO; ++i) { o[n][i][e] *= f; o[n][i][2 + e] *= f; }
                     }
-            }
-            uint32_t pb[kSub][NQ][2];
-#pragma unroll
-            for (int s = 0; s < kSub; ++s)
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) {
-                    const float p0 = ex2(fmaf(sc[s][n][0], scale, -ref[n][0])), p1 = ex2(fmaf(sc[s][n][1], scale, -ref[n][1]));
-                    const float p2 = ex2(fmaf(sc[s][n][2], scale, -ref[n][0])), p3 = ex2(fmaf(sc[s][n][3], scale, -ref[n][1]));
-                    l[n][0] += p0 + p2;
-                    l[n][1] += p1 + p3;
-                    pb[s][n][0] = transpose8(pack_bf16(p0, p1));
-                    pb[s][n][1] = transpose8(pack_bf16(p2, p3));
                 }
+        }
+        uint32_t pb[kSub][NQ][2];
 #pragma unroll
-            for (int s = 0; s < kSub; ++s) {
-                const uint32_t blk = st + s * C::kBlock;
-                if constexpr (kInt4) {
-                    uint32_t va[D / 64][4], vs[kG][2];      // [h][key 2 t, 2 t + 1, 2 t + 8, 2 t + 9]
-                    const uint32_t vt = blk + Block4<D>::offV, vsc = blk + Block4<D>::offVS;
-                    if constexpr (D == 128) {
-                        const uint4 x = lds128(vt + lane * 16), y = lds128(vt + 512 + lane * 16), z = lds128(vsc + t4 * 32), w = lds128(vsc + t4 * 32 + 16);
-                        va[0][0] = x.x; va[1][0] = x.y; va[0][1] = x.z; va[1][1] = x.w;
-                        va[0][2] = y.x; va[1][2] = y.y; va[0][3] = y.z; va[1][3] = y.w;
-                        vs[0][0] = z.x; vs[0][1] = z.y; vs[1][0] = z.z; vs[1][1] = z.w;
-                        vs[2][0] = w.x; vs[2][1] = w.y; vs[3][0] = w.z; vs[3][1] = w.w;
+        for (int s = 0; s < kSub; ++s)
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                const float p0 = ex2(fmaf(sc[s][n][0], scale, -ref[n][0])), p1 = ex2(fmaf(sc[s][n][1], scale, -ref[n][1]));
+                const float p2 = ex2(fmaf(sc[s][n][2], scale, -ref[n][0])), p3 = ex2(fmaf(sc[s][n][3], scale, -ref[n][1]));
+                l[n][0] += p0 + p2;
+                l[n][1] += p1 + p3;
+                pb[s][n][0] = transpose8(pack_bf16(p0, p1));
+                pb[s][n][1] = transpose8(pack_bf16(p2, p3));
+            }
+#pragma unroll
+        for (int s = 0; s < kSub; ++s) values(pb[s], st + s * kBlock, lane, ragged, here >> s & 1 ? left - 16 * s : 0);
+    }
+
+    // Eight queries (the n-th eight) of this warp into the merge: rows of kLd floats, and (maximum, sum) of each
+    __device__ __forceinline__ void leave(int n, int rows, float *merge, float2 *ml, int warp, int lane) const
+    {
+        constexpr int kLd = Cfg<D, kInt4, NQ>::kLd;
+        const int g = lane / 4, t4 = lane % 4;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float lt = l[n][e];
+            lt += __shfl_xor_sync(0xffffffffu, lt, 4);
+            lt += __shfl_xor_sync(0xffffffffu, lt, 8);
+            lt += __shfl_xor_sync(0xffffffffu, lt, 16);
+            const int r = 2 * t4 + e;
+            if (r < rows) {
+                float *row = merge + (warp * 8 + r) * kLd;
+#pragma unroll
+                for (int i = 0; i < kNO; ++i) {
+                    if constexpr (kInt4) {
+                        constexpr float k0 = exp2i(-kCodeExp0 - kLift), k1 = exp2i(-kCodeExp1 - kLift);
+                        if (i % 2 == 0)
+                            *reinterpret_cast<float4 *>(row + 16 * i + 4 * g) =
+                                make_float4(k0 * o[n][i][e], k1 * o[n][i][2 + e], k0 * o[n][i + 1][e], k1 * o[n][i + 1][2 + e]);
                     } else {
-                        const uint2 x = lds64(vt + lane * 8), y = lds64(vt + 256 + lane * 8);
-                        const uint4 z = lds128(vsc + t4 * 16);
-                        va[0][0] = x.x; va[0][1] = x.y; va[0][2] = y.x; va[0][3] = y.y;
-                        vs[0][0] = z.x; vs[0][1] = z.y; vs[1][0] = z.z; vs[1][1] = z.w;
-                    }
-                    if (ragged) {      // past the end: weights of 0, and whatever the scales there are (they may not be numbers)
-                        const int in = here >> s & 1 ? left - 16 * s : 0, k = 2 * t4;
-                        const uint32_t m0 = (k < in ? 0xffffu : 0u) | (k + 1 < in ? 0xffff0000u : 0u), m1 = (k + 8 < in ? 0xffffu : 0u) | (k + 9 < in ? 0xffff0000u : 0u);
-#pragma unroll
-                        for (int y = 0; y < kG; ++y) { vs[y][0] &= m0; vs[y][1] &= m1; }
-                    }
-#pragma unroll
-                    for (int y = 0; y < kG; ++y) {
-                        const uint32_t sel = y % 2 ? 0x7632u : 0x5410u;
-                        const uint32_t w01 = __byte_perm(va[y / 2][0], va[y / 2][1], sel), w23 = __byte_perm(va[y / 2][2], va[y / 2][3], sel);
-                        uint32_t b0[NQ], b1[NQ];
-#pragma unroll
-                        for (int n = 0; n < NQ; ++n) { b0[n] = mul2(pb[s][n][0], vs[y][0]); b1[n] = mul2(pb[s][n][1], vs[y][1]); }
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const uint32_t x01 = u ? w01 >> 8 : w01, x23 = u ? w23 >> 8 : w23;
-                            uint32_t v[4];
-                            v[0] = add2(nibbles(x01, 0), 0x80088008u);          // - 8
-                            v[1] = add2(nibbles(x01, 1), 0x80808080u);
-                            v[2] = add2(nibbles(x23, 0), 0x80088008u);
-                            v[3] = add2(nibbles(x23, 1), 0x80808080u);
-#pragma unroll
-                            for (int n = 0; n < NQ; ++n) mma16816(o[n][2 * y + u], v, b0[n], b1[n]);
-                        }
-                    }
-                } else {
-                    const int r = (lane / 16) * 8 + lane % 8;
-#pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        const int c = 2 * i + (lane / 8 & 1);
-                        uint32_t v[4];
-                        ldmatrix4_trans(v, blk + 32 * D + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16);
-#pragma unroll
-                        for (int n = 0; n < NQ; ++n) mma16816(o[n][i], v, pb[s][n][0], pb[s][n][1]);
+                        row[16 * i + g] = o[n][i][e];
+                        row[16 * i + 8 + g] = o[n][i][2 + e];
                     }
                 }
+                if (g == 0) ml[warp * 8 + r] = make_float2(top[n][e] == -INFINITY ? -INFINITY : ref[n][e] + kUp, lt * exp2i(-(int)kUp));
             }
         }
-        // ---- the segment's end: the warps' results joined, eight queries at a time
+    }
+};
+
+// The end of a segment of a head (the warps that compute, all of them): their results joined, eight queries at a time, and written: the head's result
+// (whole), or a partial one
+template <int D, bool kInt4, int NQ>
+__device__ __forceinline__ void join(const PagedArgs &a, const HeadState<D, kInt4, NQ> &s, uint8_t *smem, int head, bool whole, int slot)
+{
+    using C = Cfg<D, kInt4, NQ>;
+    constexpr int kJoin = 32 * kWarps;
+    float *merge = reinterpret_cast<float *>(smem + C::offMerge);
+    float2 *ml = reinterpret_cast<float2 *>(smem + C::offMl);
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int rows = min(8, a.G - 8 * n);
+        named_barrier(1, kJoin);                // (the join before has been read)
+        s.leave(n, rows, merge, ml, tid / 32, tid % 32);
+        named_barrier(1, kJoin);
+        for (int idx = tid; idx < rows * (D / 4); idx += kJoin) {
+            const int r = idx / (D / 4), c = 4 * (idx % (D / 4));
+            float mt = -INFINITY, ls = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) mt = fmaxf(mt, ml[w * 8 + r].x);
+            const float ref = mt == -INFINITY ? 0.f : mt;
+            float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float2 x = ml[w * 8 + r];
+                const float f = ex2(x.x - ref);
+                const float4 v = *reinterpret_cast<const float4 *>(merge + (w * 8 + r) * C::kLd + c);
+                ls = fmaf(x.y, f, ls);
+                ot.x = fmaf(v.x, f, ot.x); ot.y = fmaf(v.y, f, ot.y); ot.z = fmaf(v.z, f, ot.z); ot.w = fmaf(v.w, f, ot.w);
+            }
+            if (whole) {
+                const size_t at = (size_t)head * a.G + 8 * n + r;
+                const float inv = ls == 0.f ? 0.f : 1.f / ls;
+                *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
+                if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + log2f(ls)) * kLn2;
+            } else {
+                const size_t at = (size_t)slot * a.G + 8 * n + r;
+                *reinterpret_cast<float4 *>(a.part_o + at * D + c) = ot;
+                if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(mt, ls);
+            }
+        }
+    }
+}
+
+// The segments of a share in turn: `next` makes a step of this warp with the head's state
+template <int D, bool kInt4, int NQ, class Next>
+__device__ __forceinline__ void walk(const PagedArgs &a, const Share &sh, Place<Cfg<D, kInt4, NQ>> use, const __nv_bfloat16 *q, const int *lens, uint8_t *smem, Next next)
+{
+    const int count = sh.u1 - sh.u0, lane = threadIdx.x % 32;
+    int done = 0;
+    int2 told = make_int2(-1, 0);
+    HeadState<D, kInt4, NQ> s;
+    while (done < count) {
+        const int first = use.t, steps = min(use.end - use.t, count - done), head = use.b * a.Hkv + use.h;
+        s.begin(a, q, use.b, use.h, lane);
+        for (int i = 0; i < steps; ++i, ++done, ++use.t) next(s, use);
         const bool whole = first == 0 && use.t == use.end;
-        const int slot = 2 * (int)blockIdx.x + (first == 0 ? 1 : 0);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            const int rows = min(8, a.G - 8 * n);
-            __syncthreads();                // (the join before has been read)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float lt = l[n][e];
-                lt += __shfl_xor_sync(0xffffffffu, lt, 4);
-                lt += __shfl_xor_sync(0xffffffffu, lt, 8);
-                lt += __shfl_xor_sync(0xffffffffu, lt, 16);
-                const int r = 2 * t4 + e;
-                if (r < rows) {
-                    float *row = merge + (warp * 8 + r) * C::kLd;
-#pragma unroll
-                    for (int i = 0; i < C::kNO; ++i) {
-                        if constexpr (kInt4) {
-                            constexpr float k0 = exp2i(-kCodeExp0 - kLift), k1 = exp2i(-kCodeExp1 - kLift);
-                            if (i % 2 == 0)
-                                *reinterpret_cast<float4 *>(row + 16 * i + 4 * g) =
-                                    make_float4(k0 * o[n][i][e], k1 * o[n][i][2 + e], k0 * o[n][i + 1][e], k1 * o[n][i + 1][2 + e]);
-                        } else {
-                            row[16 * i + g] = o[n][i][e];
-                            row[16 * i + 8 + g] = o[n][i][2 + e];
-                        }
-                    }
-                    if (g == 0) ml[warp * 8 + r] = make_float2(top[n][e] == -INFINITY ? -INFINITY : ref[n][e] + kUp, lt * exp2i(-(int)kUp));
-                }
-            }
-            __syncthreads();
-            for (int idx = tid; idx < rows * (D / 4); idx += kThreads) {
-                const int r = idx / (D / 4), c = 4 * (idx % (D / 4));
-                float mt = -INFINITY, ls = 0.f;
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) mt = fmaxf(mt, ml[w * 8 + r].x);
-                const float ref = mt == -INFINITY ? 0.f : mt;
-                float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) {
-                    const float2 x = ml[w * 8 + r];
-                    const float f = ex2(x.x - ref);
-                    const float4 v = *reinterpret_cast<const float4 *>(merge + (w * 8 + r) * C::kLd + c);
-                    ls = fmaf(x.y, f, ls);
-                    ot.x = fmaf(v.x, f, ot.x); ot.y = fmaf(v.y, f, ot.y); ot.z = fmaf(v.z, f, ot.z); ot.w = fmaf(v.w, f, ot.w);
-                }
-                if (whole) {
-                    const size_t at = (size_t)head * a.G + 8 * n + r;
-                    const float inv = ls == 0.f ? 0.f : 1.f / ls;
-                    *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
-                    if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + log2f(ls)) * kLn2;
-                } else {
-                    const size_t at = (size_t)slot * a.G + 8 * n + r;
-                    *reinterpret_cast<float4 *>(a.part_o + at * D + c) = ot;
-                    if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(mt, ls);
-                }
-            }
-        }
+        join<D, kInt4, NQ>(a, s, smem, head, whole, 2 * (int)blockIdx.x + (first == 0 ? 1 : 0));
         if (!whole && first == 0) {
             // the head's last unit, and whose share that is in
             const int last = sh.u0 + done - use.t + use.end - 1;
@@ -598,11 +543,187 @@ __global__ void __launch_bounds__(kThreads, (Cfg<D, kInt4, NQ>::kCtas)) paged_de
         if (use.t == use.end) {
             int b = use.b, h = use.h + 1;
             if (h == a.Hkv) { h = 0; ++b; }
-            use.set(b, h, 0, b == use.b ? use.len : length(b));
+            use.set(b, h, 0, b == use.b ? use.len : length_of(a, lens, b));
         }
     }
+    if (threadIdx.x == 0) a.info[blockIdx.x] = told;
+}
+
+template <int D, int NQ>
+__global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ>::kCtas)) paged_decode4_kernel(const PagedArgs a)
+{
+    using C = Cfg<D, true, NQ>;
+    constexpr int S = C::kStages, kUnit = C::kBlocks * C::kBlock;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint64_t *full = reinterpret_cast<uint64_t *>(smem + C::offBar), *empty = full + S;
+    volatile uint32_t *live = reinterpret_cast<uint32_t *>(empty + S), *abortp = live + S;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
+    if (tid == 0) {
+        for (int s = 0; s < S; ++s) { mbar_init(full + s, 1); mbar_init(empty + s, kWarps); }
+        *abortp = 0;
+        fence_mbar_init();
+    }
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int *lens = after_wait(a.lens), *table = after_wait(a.table);
+    const Share sh = find_share<C>(a, lens, reinterpret_cast<int *>(smem + C::offScan));      // (its barriers are those of the set-up too)
+    const int count = sh.u1 - sh.u0;
+    if (count == 0) {
+        if (tid == 0) a.info[blockIdx.x] = make_int2(-1, 0);
+        return;
+    }
+    Place<C> at;
+    {
+        const int len = length_of(a, lens, sh.b), end = units_of<C::kUnitKeys>(len), in = sh.u0 - sh.before;
+        at.set(sh.b, in / end, in % end, len);
+    }
+
+    if (warp == kWarps) {
+        // ------------------------------------------------------------------ loads: a lane per block, four units to a batch of table entries
+        constexpr int kBatch = 32 / C::kBlocks;
+        const uint8_t *pool = after_wait(a.pool);
+        const int mine = lane / C::kBlocks, block = lane % C::kBlocks;
+        ArmCounts<S> armed;
+        int base = at.t, nb, nh, nlen, stage = 0, round = 0;
+        long long cur = block_offset<D, true, C>(a, table, at.b, at.h, base + mine, block), nxt;
+        auto fetch_next = [&] {      // the batch behind the current one
+            nb = at.b; nh = at.h; nlen = at.len;
+            int nt = base + kBatch;
+            if (nt >= at.end) {
+                nt = 0;
+                if (++nh == a.Hkv) { nh = 0; nlen = length_of(a, lens, ++nb); }
+            }
+            nxt = block_offset<D, true, C>(a, table, nb, nh, nt + mine, block);
+        };
+        fetch_next();
+        for (int i = 0; i < count; ++i) {
+            bool ok = round == 0 || mbar_wait(empty + stage, (round - 1) & 1, abortp, a.status, PERR_EMPTY);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const bool valid = mine == at.t - base && cur >= 0 && at.t * C::kUnitKeys + 16 * block < at.len;
+            const uint32_t who = __ballot_sync(0xffffffffu, valid);
+            if (lane == 0) {
+                live[stage] = who >> ((at.t - base) * C::kBlocks);
+                mbar_arm(full, stage, (uint32_t)(__popc(who) * C::kBlock), armed);
+            }
+            __syncwarp();
+            if (valid) bulk_load_1d(smem + stage * kUnit + block * C::kBlock, pool + cur, C::kBlock, full + stage);
+            if (++stage == S) { stage = 0; ++round; }
+            ++at.t;
+            const bool over = at.t == at.end;
+            if (over || at.t == base + kBatch) {
+                if (over) at.set(nb, nh, 0, nlen);
+                base = at.t;
+                cur = nxt;
+                fetch_next();
+            }
+        }
+        if (lane == 0) mbar_drain(full, armed);      // copies still on their way land before the CTA leaves (bounded)
+        return;
+    }
+
+    // ---------------------------------------------------------------------- use
+    const float scale = a.scale_log2 * exp2i(-kCodeExp1 - kLift), margin = kRescale / scale;
+    const uint32_t ring = smem_u32(smem);
+    int stage = 0, parity = 0;
+    bool ok = true;
+    walk<D, true, NQ>(a, sh, at, after_wait(a.q), lens, smem, [&](HeadState<D, true, NQ> &s, const Place<C> &use) {
+        if (ok && !mbar_wait(full + stage, parity, abortp, a.status, PERR_FULL)) ok = false;
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return;
+        const uint32_t here = live[stage] >> (C::kSub * warp) & ((1u << C::kSub) - 1);
+        if (here) s.step(ring + stage * kUnit + warp * C::kSub * C::kBlock, here, use.len - (use.t * C::kUnitKeys + 16 * C::kSub * warp), scale, margin, lane);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty + stage);
+        if (++stage == S) { stage = 0; parity ^= 1; }
+    });
+}
+
+template <int D, int NQ>
+__global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, NQ>::kCtas)) paged_decode16_kernel(const PagedArgs a)
+{
+    using C = Cfg<D, false, NQ>;
+    constexpr int S = C::kStages;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int *lens = after_wait(a.lens), *table = after_wait(a.table);
+    const uint8_t *pool = after_wait(a.pool);
+    const Share sh = find_share<C>(a, lens, reinterpret_cast<int *>(smem + C::offScan));
+    const int count = sh.u1 - sh.u0;
+    if (count == 0) {
+        if (tid == 0) a.info[blockIdx.x] = make_int2(-1, 0);
+        return;
+    }
+    Place<C> ask;
+    {
+        const int len = length_of(a, lens, sh.b), end = units_of<C::kUnitKeys>(len), in = sh.u0 - sh.before;
+        ask.set(sh.b, in / end, in % end, len);
+    }
+    const Place<C> start = ask;
+
+    // ---- requests: S - 1 steps ahead of their use
+    const uint32_t ring = smem_u32(smem) + warp * S * C::kBlock;
+    int left_to_ask = count, base = ask.t, nb, nh, nlen;      // base: unit of the batch's first entry
+    uint32_t live = 0;                                        // stages that hold keys
+    long long cur = block_offset<D, false, C>(a, table, ask.b, ask.h, base + lane, warp), nxt;
+    auto fetch_next = [&] {      // the batch behind the current one
+        nb = ask.b; nh = ask.h; nlen = ask.len;
+        int nt = base + 32;
+        if (nt >= ask.end) {
+            nt = 0;
+            if (++nh == a.Hkv) { nh = 0; nlen = length_of(a, lens, ++nb); }
+        }
+        nxt = block_offset<D, false, C>(a, table, nb, nh, nt + lane, warp);
+    };
+    fetch_next();
+    auto request = [&](int stage) {
+        live &= ~(1u << stage);
+        if (left_to_ask > 0) {
+            --left_to_ask;
+            const long long at = __shfl_sync(0xffffffffu, cur, ask.t - base);
+            const int left = ask.len - (ask.t * C::kUnitKeys + 16 * warp);
+            if (at >= 0 && left > 0) {
+                // rows past the end of the sequence are filled with zeros: whatever they hold, their weight is 0
+                constexpr int kRow = D / 8, kAt = 32 / kRow;
+                const int c = lane % kRow;
+                live |= 1u << stage;
+#pragma unroll
+                for (int i = 0; i < 16 / kAt; ++i) {
+                    const int r = i * kAt + lane / kRow, bytes = r < left ? 16 : 0;
+                    const uint32_t to = ring + stage * C::kBlock + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16;
+                    const uint8_t *from = pool + at + (bytes ? r * (2 * D) + c * 16 : 0);
+                    cp_async16(to, from, bytes);
+                    cp_async16(to + 32 * D, from + (long long)a.page * (2 * D), bytes);
+                }
+            }
+            ++ask.t;
+            const bool over = ask.t == ask.end;
+            if (over || ask.t == base + 32) {
+                if (over) ask.set(nb, nh, 0, nlen);
+                base = ask.t;
+                cur = nxt;
+                fetch_next();
+            }
+        }
+        cp_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) request(i);
+
+    // ---- use
+    const float margin = kRescale / a.scale_log2;
+    int get = 0;      // stage of this step
+    walk<D, false, NQ>(a, sh, start, after_wait(a.q), lens, smem, [&](HeadState<D, false, NQ> &s, const Place<C> &use) {
+        cp_wait<S - 2>();
+        __syncwarp();
+        const uint32_t st = ring + get * C::kBlock, here = live >> get & 1;
+        request(get == 0 ? S - 1 : get - 1);      // (into the stage of the step before)
+        get = get == S - 1 ? 0 : get + 1;
+        if (here) s.step(st, here, use.len - (use.t * C::kUnitKeys + 16 * warp), a.scale_log2, margin, lane);
+    });
     cp_wait<0>();
-    if (tid == 0) a.info[blockIdx.x] = told;
 }
 
 // Heads that lie in several shares: block (c, query) joins the partial results of the head that begins in share c and goes on, its 128 threads in
@@ -686,7 +807,8 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
                    cudaStream_t st)
 {
     using C = Cfg<D, kInt4, NQ>;
-    const cudaError_t e = allow_smem<paged_decode_kernel<D, kInt4, NQ>>(C::kTotal);
+    constexpr auto kernel = [] { if constexpr (kInt4) return paged_decode4_kernel<D, NQ>; else return paged_decode16_kernel<D, NQ>; }();
+    const cudaError_t e = allow_smem<kernel>(C::kTotal);
     if (e != cudaSuccess) return e;
     const int G = p.H / p.pool.Hkv, ctas = ctas_for(p, C::kCtas, C::kUnitKeys), most = 4 * device_info().sms;
     PagedArgs a{};
@@ -700,11 +822,12 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     a.B = p.B; a.Hkv = p.pool.Hkv; a.G = G; a.pages = p.pool.pages; a.page = p.pool.page;
     a.cap = (int)((long long)p.max_pages * p.pool.page);
     a.by_page = FastDiv((uint32_t)p.pool.page);
+    a.status = device_status_ptr();
     a.scale_log2 = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
     a.sign2 = p.scale == 0.f ? 0u : p.scale > 0.f ? 0x3f803f80u : 0xbf80bf80u;
     {
         LaunchScope scope(MOA_KERNEL_OTHER, st);
-        const cudaError_t le = launch_dependent(paged_decode_kernel<D, kInt4, NQ>, dim3((unsigned)ctas), dim3(kThreads), (size_t)C::kTotal, st, a);
+        const cudaError_t le = launch_dependent(kernel, dim3((unsigned)ctas), dim3(C::kThreads), (size_t)C::kTotal, st, a);
         if (le != cudaSuccess) return le;
     }
     LaunchScope scope(MOA_KERNEL_OTHER, st);
