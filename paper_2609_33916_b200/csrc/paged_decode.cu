@@ -20,6 +20,7 @@
 // joins them: CTA c tells it which head begins in its share and goes on, and where that ends.
 #include "cache_layout.cuh"
 #include "ptx.cuh"
+#include <algorithm>
 
 namespace moa {
 namespace {
@@ -37,7 +38,7 @@ struct PagedArgs {
     const int *table, *lens;
     __nv_bfloat16 *out;
     float *lse, *part_o, *part_ml;
-    int2 *info;                 // per CTA: the head that begins in its share and goes on (-1: none), the CTA that ends it
+    int2 *info;                 // of a share: the head that begins in it and goes on (-1: none), the share that ends it
     RopeStride sq;
     long long table_stride, page_stride;
     int B, Hkv, G, pages, page, cap;      // cap: keys that a row of the table has room for
@@ -49,18 +50,22 @@ struct PagedArgs {
 
 template <int D, bool kInt4, int NQ>
 struct Cfg {
-    static constexpr int kThreads = 32 * (kWarps + (kInt4 ? 1 : 0));
+    static constexpr int kTeams = kInt4 ? (NQ == 2 ? 2 : 3) : 1;                       // of kWarps warps, with a share of the work each
+    static constexpr int kThreads = 128 * (kTeams + (kInt4 ? 1 : 0));
     static constexpr int kSub = kInt4 ? 2 : 1;                                         // blocks of 16 keys that a warp takes in a step
     static constexpr int kBlocks = kSub * kWarps, kUnitKeys = 16 * kBlocks;
     static constexpr int kBlock = kInt4 ? Block4<D>::kBytes : 16 * D * 4;
-    static constexpr int kCtas = NQ == 2 ? 2 : kInt4 || D == 64 ? 3 : 2;               // resident per SM
+    static constexpr int kCtas = kInt4 ? 1 : NQ == 2 || D == 128 ? 2 : 3;              // resident per SM
+    static constexpr int kShares = kCtas * kTeams;                                     // per SM
     static constexpr int kStages = kInt4 ? (D == 64 ? 6 : NQ == 2 ? 4 : 3) : D == 128 ? 3 : 4;
     static constexpr int kLd = D + 4;                                                  // floats of a row of the merge
+    // shared memory of a team
     static constexpr int offMerge = kStages * kBlocks * kBlock;
     static constexpr int offMl = offMerge + kWarps * 8 * kLd * 4;                      // [warps][8] (maximum, sum)
     static constexpr int offBar = offMl + kWarps * 8 * 8;                              // full, empty [stages], then [stages] words: blocks that hold keys
-    static constexpr int offScan = offBar + kStages * 20 + 4;
-    static constexpr int kTotal = (offScan + 48 + 15) / 16 * 16;
+    static constexpr int kTeam = (offBar + kStages * 20 + 4 + 127) / 128 * 128;
+    static constexpr int offScan = kTeams * kTeam;                                     // of the CTA: 16 words of sums, two for each team
+    static constexpr int kTotal = offScan + 128;
     static constexpr int kNO = D / 16;                                                 // tiles of O^T
 };
 
@@ -130,15 +135,17 @@ __device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w
 __device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 template <int kUnitKeys> __device__ __forceinline__ int units_of(int len) { return len > 0 ? (len + kUnitKeys - 1) / kUnitKeys : 1; }
-__device__ __forceinline__ int first_unit(int units, int c, int ctas) { return (int)((long long)units * c / ctas); }
+__device__ __forceinline__ int first_unit(int units, int c, int shares) { return (int)((long long)units * c / shares); }
 
-// The share of CTA c: units [u0, u1) of `units`, and the sequence that holds u0 with the units in front of it
+// Shares, one for each team of the grid: share c is units [first_unit(c), first_unit(c + 1)) of `units`.  Team k of CTA b has share k * gridDim + b, so that
+// the first teams of all CTAs come first.
 struct Share {
-    int units, ctas, u0, u1, b, before;
+    int units, shares, c, u0, u1, b, before;      // b: the sequence that holds u0; before: units in front of it
 };
-template <class C> __device__ __forceinline__ Share find_share(const PagedArgs &a, const int *lens, int *scan)
+template <class C> __device__ __forceinline__ Share find_share(const PagedArgs &a, const int *lens, int *scan, int team)
 {
     constexpr int kThreads = C::kThreads, kAll = kThreads / 32;
+    static_assert(kAll <= 16, "a warp's sum each");
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     Share s;
     int sum = 0, first = 0;
@@ -154,14 +161,11 @@ template <class C> __device__ __forceinline__ Share find_share(const PagedArgs &
 #pragma unroll
     for (int w = 0; w < kAll; ++w) sum += scan[w];
     s.units = sum * a.Hkv;
-    s.ctas = min((int)gridDim.x, s.units);
-    const int c = blockIdx.x;
-    s.u0 = c < s.ctas ? first_unit(s.units, c, s.ctas) : s.units;
-    s.u1 = c < s.ctas ? first_unit(s.units, c + 1, s.ctas) : s.units;
-    s.b = s.before = 0;
-    if (s.u0 == s.u1) return s;
-    const int row = s.u0 / a.Hkv;      // units of one head: the sequence is the one whose sum passes this (all heads have the same)
-    int carry = 0;
+    s.shares = min((int)gridDim.x * C::kTeams, s.units);
+    auto begin_of = [&](int c) { return c < s.shares ? first_unit(s.units, c, s.shares) : s.units; };
+    int row[C::kTeams], carry = 0;      // where each team's share begins, in units of one head (all heads have the same)
+#pragma unroll
+    for (int k = 0; k < C::kTeams; ++k) row[k] = begin_of(k * (int)gridDim.x + (int)blockIdx.x) / a.Hkv;
     for (int b0 = 0; b0 < a.B; b0 += kThreads) {
         const int b = b0 + tid, n = b0 == 0 ? first : b < a.B ? units_of<C::kUnitKeys>(min(lens[b], a.cap)) : 0;
         int incl = n;
@@ -179,13 +183,18 @@ template <class C> __device__ __forceinline__ Share find_share(const PagedArgs &
             all += scan[w];
         }
         incl += carry;
-        if (incl - n <= row && row < incl) { scan[kAll] = b; scan[kAll + 1] = incl - n; }
+#pragma unroll
+        for (int k = 0; k < C::kTeams; ++k)
+            if (incl - n <= row[k] && row[k] < incl) { scan[16 + 2 * k] = b; scan[17 + 2 * k] = incl - n; }
         carry += all;
-        if (carry > row) break;      // (the same in every thread)
+        if (carry > row[C::kTeams - 1]) break;      // (the same in every thread; the last team's is the last)
     }
     __syncthreads();
-    s.b = scan[kAll];
-    s.before = scan[kAll + 1] * a.Hkv;
+    s.c = team * (int)gridDim.x + (int)blockIdx.x;
+    s.u0 = begin_of(s.c);
+    s.u1 = begin_of(s.c + 1);
+    s.b = s.u0 < s.u1 ? scan[16 + 2 * team] : 0;
+    s.before = s.u0 < s.u1 ? scan[17 + 2 * team] * a.Hkv : 0;
     return s;
 }
 
@@ -477,19 +486,19 @@ struct HeadState {
 // The end of a segment of a head (the warps that compute, all of them): their results joined, eight queries at a time, and written: the head's result
 // (whole), or a partial one
 template <int D, bool kInt4, int NQ>
-__device__ __forceinline__ void join(const PagedArgs &a, const HeadState<D, kInt4, NQ> &s, uint8_t *smem, int head, bool whole, int slot)
+__device__ __forceinline__ void join(const PagedArgs &a, const HeadState<D, kInt4, NQ> &s, uint8_t *smem, int team, int head, bool whole, int slot)
 {
     using C = Cfg<D, kInt4, NQ>;
     constexpr int kJoin = 32 * kWarps;
     float *merge = reinterpret_cast<float *>(smem + C::offMerge);
     float2 *ml = reinterpret_cast<float2 *>(smem + C::offMl);
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x % kJoin;
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         const int rows = min(8, a.G - 8 * n);
-        named_barrier(1, kJoin);                // (the join before has been read)
+        named_barrier(1 + team, kJoin);                // (the join before has been read)
         s.leave(n, rows, merge, ml, tid / 32, tid % 32);
-        named_barrier(1, kJoin);
+        named_barrier(1 + team, kJoin);
         for (int idx = tid; idx < rows * (D / 4); idx += kJoin) {
             const int r = idx / (D / 4), c = 4 * (idx % (D / 4));
             float mt = -INFINITY, ls = 0.f;
@@ -521,7 +530,7 @@ __device__ __forceinline__ void join(const PagedArgs &a, const HeadState<D, kInt
 
 // The segments of a share in turn: `next` makes a step of this warp with the head's state
 template <int D, bool kInt4, int NQ, class Next>
-__device__ __forceinline__ void walk(const PagedArgs &a, const Share &sh, Place<Cfg<D, kInt4, NQ>> use, const __nv_bfloat16 *q, const int *lens, uint8_t *smem, Next next)
+__device__ __forceinline__ void walk(const PagedArgs &a, const Share &sh, Place<Cfg<D, kInt4, NQ>> use, const __nv_bfloat16 *q, const int *lens, uint8_t *smem, int team, Next next)
 {
     const int count = sh.u1 - sh.u0, lane = threadIdx.x % 32;
     int done = 0;
@@ -532,12 +541,12 @@ __device__ __forceinline__ void walk(const PagedArgs &a, const Share &sh, Place<
         s.begin(a, q, use.b, use.h, lane);
         for (int i = 0; i < steps; ++i, ++done, ++use.t) next(s, use);
         const bool whole = first == 0 && use.t == use.end;
-        join<D, kInt4, NQ>(a, s, smem, head, whole, 2 * (int)blockIdx.x + (first == 0 ? 1 : 0));
+        join<D, kInt4, NQ>(a, s, smem, team, head, whole, 2 * sh.c + (first == 0 ? 1 : 0));
         if (!whole && first == 0) {
             // the head's last unit, and whose share that is in
             const int last = sh.u0 + done - use.t + use.end - 1;
-            int c = (int)((long long)last * sh.ctas / sh.units);
-            while (first_unit(sh.units, c + 1, sh.ctas) <= last) ++c;
+            int c = (int)((long long)last * sh.shares / sh.units);
+            while (first_unit(sh.units, c + 1, sh.shares) <= last) ++c;
             told = make_int2(head, c);
         }
         if (use.t == use.end) {
@@ -546,7 +555,7 @@ __device__ __forceinline__ void walk(const PagedArgs &a, const Share &sh, Place<
             use.set(b, h, 0, b == use.b ? use.len : length_of(a, lens, b));
         }
     }
-    if (threadIdx.x == 0) a.info[blockIdx.x] = told;
+    if (threadIdx.x % (32 * kWarps) == 0) a.info[sh.c] = told;
 }
 
 template <int D, int NQ>
@@ -554,11 +563,16 @@ __global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ
 {
     using C = Cfg<D, true, NQ>;
     constexpr int S = C::kStages, kUnit = C::kBlocks * C::kBlock;
-    extern __shared__ __align__(1024) uint8_t smem[];
+    // registers of a thread that computes and of one that loads: 128 (384 threads: 168) at launch, 3 x 152 + 56 = 4 x 128, 2 x 224 + 56 = 3 x 168
+    constexpr int kUseRegs = NQ == 2 ? 224 : 152, kLoadRegs = 56;
+    extern __shared__ __align__(1024) uint8_t shared[];
+    const bool loads = (int)threadIdx.x >= 128 * C::kTeams;
+    const int team = __shfl_sync(0xffffffffu, loads ? (int)threadIdx.x / 32 - kWarps * C::kTeams : (int)threadIdx.x / 128, 0);      // (the fourth loading warp: none)
+    uint8_t *smem = shared + min(team, C::kTeams - 1) * C::kTeam;
     uint64_t *full = reinterpret_cast<uint64_t *>(smem + C::offBar), *empty = full + S;
     volatile uint32_t *live = reinterpret_cast<uint32_t *>(empty + S), *abortp = live + S;
-    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
-    if (tid == 0) {
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32 % kWarps, 0), lane = tid % 32;
+    if (!loads && tid % 128 == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(full + s, 1); mbar_init(empty + s, kWarps); }
         *abortp = 0;
         fence_mbar_init();
@@ -566,19 +580,17 @@ __global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ
     grid_dependency_wait();
     grid_launch_dependents();
     const int *lens = after_wait(a.lens), *table = after_wait(a.table);
-    const Share sh = find_share<C>(a, lens, reinterpret_cast<int *>(smem + C::offScan));      // (its barriers are those of the set-up too)
+    const Share sh = find_share<C>(a, lens, reinterpret_cast<int *>(shared + C::offScan), min(team, C::kTeams - 1));      // (its barriers are those of the set-up too)
     const int count = sh.u1 - sh.u0;
-    if (count == 0) {
-        if (tid == 0) a.info[blockIdx.x] = make_int2(-1, 0);
-        return;
-    }
-    Place<C> at;
-    {
+    Place<C> at{};
+    if (count > 0) {
         const int len = length_of(a, lens, sh.b), end = units_of<C::kUnitKeys>(len), in = sh.u0 - sh.before;
         at.set(sh.b, in / end, in % end, len);
     }
 
-    if (warp == kWarps) {
+    if (loads) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
+        if (team >= C::kTeams || count == 0) return;
         // ------------------------------------------------------------------ loads: a lane per block, four units to a batch of table entries
         constexpr int kBatch = 32 / C::kBlocks;
         const uint8_t *pool = after_wait(a.pool);
@@ -624,10 +636,11 @@ __global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ
 
     // ---------------------------------------------------------------------- use
     const float scale = a.scale_log2 * exp2i(-kCodeExp1 - kLift), margin = kRescale / scale;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kUseRegs));
     const uint32_t ring = smem_u32(smem);
     int stage = 0, parity = 0;
     bool ok = true;
-    walk<D, true, NQ>(a, sh, at, after_wait(a.q), lens, smem, [&](HeadState<D, true, NQ> &s, const Place<C> &use) {
+    walk<D, true, NQ>(a, sh, at, after_wait(a.q), lens, smem, team, [&](HeadState<D, true, NQ> &s, const Place<C> &use) {
         if (ok && !mbar_wait(full + stage, parity, abortp, a.status, PERR_FULL)) ok = false;
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) return;
@@ -650,10 +663,10 @@ __global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, 
     grid_launch_dependents();
     const int *lens = after_wait(a.lens), *table = after_wait(a.table);
     const uint8_t *pool = after_wait(a.pool);
-    const Share sh = find_share<C>(a, lens, reinterpret_cast<int *>(smem + C::offScan));
+    const Share sh = find_share<C>(a, lens, reinterpret_cast<int *>(smem + C::offScan), 0);
     const int count = sh.u1 - sh.u0;
     if (count == 0) {
-        if (tid == 0) a.info[blockIdx.x] = make_int2(-1, 0);
+        if (tid == 0) a.info[sh.c] = make_int2(-1, 0);
         return;
     }
     Place<C> ask;
@@ -715,7 +728,7 @@ __global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, 
     // ---- use
     const float margin = kRescale / a.scale_log2;
     int get = 0;      // stage of this step
-    walk<D, false, NQ>(a, sh, start, after_wait(a.q), lens, smem, [&](HeadState<D, false, NQ> &s, const Place<C> &use) {
+    walk<D, false, NQ>(a, sh, start, after_wait(a.q), lens, smem, 0, [&](HeadState<D, false, NQ> &s, const Place<C> &use) {
         cp_wait<S - 2>();
         __syncwarp();
         const uint32_t st = ring + get * C::kBlock, here = live >> get & 1;
@@ -795,9 +808,9 @@ paged_merge_kernel(const int2 *__restrict__ info, const float *__restrict__ part
     }
 }
 
-int ctas_for(const PagedProblem &p, int per_sm, int unit)
+int shares_for(const PagedProblem &p, int per_sm, int unit)
 {
-    // (a unit per CTA at least, at the lengths that the table has room for)
+    // (a unit for a share at least, at the lengths that the table has room for)
     const long long units = (long long)p.B * p.pool.Hkv * (((long long)p.max_pages * p.pool.page + unit - 1) / unit), most = (long long)per_sm * device_info().sms;
     return (int)(units < most ? units : most);
 }
@@ -810,7 +823,8 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     constexpr auto kernel = [] { if constexpr (kInt4) return paged_decode4_kernel<D, NQ>; else return paged_decode16_kernel<D, NQ>; }();
     const cudaError_t e = allow_smem<kernel>(C::kTotal);
     if (e != cudaSuccess) return e;
-    const int G = p.H / p.pool.Hkv, ctas = ctas_for(p, C::kCtas, C::kUnitKeys), most = 4 * device_info().sms;
+    const int G = p.H / p.pool.Hkv, sms = device_info().sms, shares = shares_for(p, C::kShares, C::kUnitKeys), most = 4 * sms;
+    const int ctas = std::min(shares, C::kCtas * sms);
     PagedArgs a{};
     a.q = (const __nv_bfloat16 *)q; a.pool = (const uint8_t *)pool; a.table = table; a.lens = lens;
     a.out = (__nv_bfloat16 *)out; a.lse = lse;
@@ -831,7 +845,7 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
         if (le != cudaSuccess) return le;
     }
     LaunchScope scope(MOA_KERNEL_OTHER, st);
-    return launch_dependent(paged_merge_kernel<D>, dim3((unsigned)ctas, (unsigned)G), dim3(128), (size_t)0, st, (const int2 *)a.info, (const float *)a.part_o,
+    return launch_dependent(paged_merge_kernel<D>, dim3((unsigned)std::min(shares, ctas * C::kTeams), (unsigned)G), dim3(128), (size_t)0, st, (const int2 *)a.info, (const float *)a.part_o,
                             (const float *)a.part_ml, (__nv_bfloat16 *)out, lse, G);
 }
 
