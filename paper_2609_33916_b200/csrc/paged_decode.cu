@@ -43,6 +43,7 @@ struct PagedArgs {
     long long table_stride, page_stride;
     int B, Hkv, G, pages, page, cap;      // cap: keys that a row of the table has room for
     FastDiv by_page;
+    int cl;                     // CTAs of a head's cluster; 0: no clusters
     float scale_log2;           // > 0; the sign (or 0) is q's factor, a pair of bf16
     uint32_t sign2;
     unsigned int *status;
@@ -195,6 +196,22 @@ template <class C> __device__ __forceinline__ Share find_share(const PagedArgs &
     s.u1 = begin_of(s.c + 1);
     s.b = s.u0 < s.u1 ? scan[16 + 2 * team] : 0;
     s.before = s.u0 < s.u1 ? scan[17 + 2 * team] * a.Hkv : 0;
+    return s;
+}
+
+// With clusters: CTA rank r of a head's cluster, team k: part r * kTeams + k of the head's units
+template <class C> __device__ __forceinline__ Share cluster_share(const PagedArgs &a, const int *lens, int team)
+{
+    Share s;
+    const int head = (int)blockIdx.x / a.cl, parts = a.cl * C::kTeams, part = (int)cluster_ctarank() * C::kTeams + team;
+    s.b = head / a.Hkv;
+    const int n = units_of<C::kUnitKeys>(min(lens[s.b], a.cap));
+    s.units = n * a.Hkv;
+    s.shares = parts;
+    s.c = part;
+    s.before = 0;
+    s.u0 = (head - s.b * a.Hkv) * n + first_unit(n, part, parts);
+    s.u1 = (head - s.b * a.Hkv) * n + first_unit(n, part + 1, parts);
     return s;
 }
 
@@ -483,9 +500,9 @@ struct HeadState {
     }
 };
 
-// The end of a segment of a head (the warps that compute, all of them): their results joined, eight queries at a time, and written: the head's result
-// (whole), or a partial one
-template <int D, bool kInt4, int NQ>
+// The end of a segment of a head (the warps of a team, all of them): their results joined, eight queries at a time, and written: the head's result
+// (whole), or a partial one; with clusters, rows of kLd floats (sums, then maximum and weights' sum) over the team's ring, which is done
+template <int D, bool kInt4, int NQ, bool kClusters>
 __device__ __forceinline__ void join(const PagedArgs &a, const HeadState<D, kInt4, NQ> &s, uint8_t *smem, int team, int head, bool whole, int slot)
 {
     using C = Cfg<D, kInt4, NQ>;
@@ -514,7 +531,11 @@ __device__ __forceinline__ void join(const PagedArgs &a, const HeadState<D, kInt
                 ls = fmaf(x.y, f, ls);
                 ot.x = fmaf(v.x, f, ot.x); ot.y = fmaf(v.y, f, ot.y); ot.z = fmaf(v.z, f, ot.z); ot.w = fmaf(v.w, f, ot.w);
             }
-            if (whole) {
+            if constexpr (kClusters) {
+                float *row = reinterpret_cast<float *>(smem) + (8 * n + r) * C::kLd;
+                *reinterpret_cast<float4 *>(row + c) = ot;
+                if (c == 0) *reinterpret_cast<float2 *>(row + D) = make_float2(mt, ls);
+            } else if (whole) {
                 const size_t at = (size_t)head * a.G + 8 * n + r;
                 const float inv = ls == 0.f ? 0.f : 1.f / ls;
                 *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
@@ -529,19 +550,26 @@ __device__ __forceinline__ void join(const PagedArgs &a, const HeadState<D, kInt
 }
 
 // The segments of a share in turn: `next` makes a step of this warp with the head's state
-template <int D, bool kInt4, int NQ, class Next>
+template <int D, bool kInt4, int NQ, bool kClusters, class Next>
 __device__ __forceinline__ void walk(const PagedArgs &a, const Share &sh, Place<Cfg<D, kInt4, NQ>> use, const __nv_bfloat16 *q, const int *lens, uint8_t *smem, int team, Next next)
 {
     const int count = sh.u1 - sh.u0, lane = threadIdx.x % 32;
     int done = 0;
-    int2 told = make_int2(-1, 0);
     HeadState<D, kInt4, NQ> s;
+    if constexpr (kClusters) {
+        s.begin(a, q, use.b, use.h, lane);
+        for (; done < count; ++done, ++use.t) next(s, use);
+        cp_wait<0>();
+        join<D, kInt4, NQ, true>(a, s, smem, team, 0, false, 0);
+        return;
+    }
+    int2 told = make_int2(-1, 0);
     while (done < count) {
         const int first = use.t, steps = min(use.end - use.t, count - done), head = use.b * a.Hkv + use.h;
         s.begin(a, q, use.b, use.h, lane);
         for (int i = 0; i < steps; ++i, ++done, ++use.t) next(s, use);
         const bool whole = first == 0 && use.t == use.end;
-        join<D, kInt4, NQ>(a, s, smem, team, head, whole, 2 * sh.c + (first == 0 ? 1 : 0));
+        join<D, kInt4, NQ, false>(a, s, smem, team, head, whole, 2 * sh.c + (first == 0 ? 1 : 0));
         if (!whole && first == 0) {
             // the head's last unit, and whose share that is in
             const int last = sh.u0 + done - use.t + use.end - 1;
@@ -558,13 +586,55 @@ __device__ __forceinline__ void walk(const PagedArgs &a, const Share &sh, Place<
     if (threadIdx.x % (32 * kWarps) == 0) a.info[sh.c] = told;
 }
 
-template <int D, int NQ>
+// A cluster's teams joined through distributed shared memory: `index` of the `threads` that compute takes its share of the head's elements.  (Between two
+// barriers of the cluster: every thread of it calls them.)
+template <int D, bool kInt4, int NQ>
+__device__ __forceinline__ void combine(const PagedArgs &a, uint8_t *shared, int index, int threads)
+{
+    using C = Cfg<D, kInt4, NQ>;
+    const int head = (int)blockIdx.x / a.cl;
+    const uint32_t base = smem_u32(shared);
+    for (int idx = index; idx < a.G * (D / 4); idx += threads) {
+        const int r = idx / (D / 4), c = 4 * (idx % (D / 4));
+        float mt = -INFINITY, ls = 0.f;
+        float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < a.cl; ++k) {
+            float2 ml[C::kTeams];
+            float4 v[C::kTeams];
+            float mn = mt;
+#pragma unroll
+            for (int j = 0; j < C::kTeams; ++j) {
+                const uint32_t row = mapa_u32(base + j * C::kTeam + r * (4 * C::kLd), (uint32_t)k);
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(ml[j].x), "=f"(ml[j].y) : "r"(row + 4 * D) : "memory");
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[j].x), "=f"(v[j].y), "=f"(v[j].z), "=f"(v[j].w) : "r"(row + 4 * c) : "memory");
+            }
+#pragma unroll
+            for (int j = 0; j < C::kTeams; ++j) mn = fmaxf(mn, ml[j].x);
+            const float ref = mn == -INFINITY ? 0.f : mn, b = ex2(mt - ref);
+            mt = mn;
+            ls *= b;
+            ot.x *= b; ot.y *= b; ot.z *= b; ot.w *= b;
+#pragma unroll
+            for (int j = 0; j < C::kTeams; ++j) {
+                const float f = ex2(ml[j].x - ref);
+                ls = fmaf(ml[j].y, f, ls);
+                ot.x = fmaf(v[j].x, f, ot.x); ot.y = fmaf(v[j].y, f, ot.y); ot.z = fmaf(v[j].z, f, ot.z); ot.w = fmaf(v[j].w, f, ot.w);
+            }
+        }
+        const size_t at = (size_t)head * a.G + r;
+        const float inv = ls == 0.f ? 0.f : 1.f / ls;
+        *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
+        if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + log2f(ls)) * kLn2;
+    }
+}
+
+template <int D, int NQ, bool kClusters>
 __global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ>::kCtas)) paged_decode4_kernel(const PagedArgs a)
 {
     using C = Cfg<D, true, NQ>;
     constexpr int S = C::kStages, kUnit = C::kBlocks * C::kBlock;
-    // registers of a thread that computes and of one that loads: 128 (384 threads: 168) at launch, 3 x 152 + 56 = 4 x 128, 2 x 224 + 56 = 3 x 168
-    constexpr int kUseRegs = NQ == 2 ? 224 : 152, kLoadRegs = 56;
+    // registers of a thread that computes and of one that loads: 128 (384 threads: 168) at launch, 3 x 160 + 32 = 4 x 128, 2 x 224 + 56 = 3 x 168
+    constexpr int kUseRegs = NQ == 2 ? 224 : 160, kLoadRegs = NQ == 2 ? 56 : 32;
     extern __shared__ __align__(1024) uint8_t shared[];
     const bool loads = (int)threadIdx.x >= 128 * C::kTeams;
     const int team = __shfl_sync(0xffffffffu, loads ? (int)threadIdx.x / 32 - kWarps * C::kTeams : (int)threadIdx.x / 128, 0);      // (the fourth loading warp: none)
@@ -580,57 +650,65 @@ __global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ
     grid_dependency_wait();
     grid_launch_dependents();
     const int *lens = after_wait(a.lens), *table = after_wait(a.table);
-    const Share sh = find_share<C>(a, lens, reinterpret_cast<int *>(shared + C::offScan), min(team, C::kTeams - 1));      // (its barriers are those of the set-up too)
+    if constexpr (kClusters) __syncthreads();                    // (else the barriers of find_share are those of the set-up too)
+    const Share sh = kClusters ? cluster_share<C>(a, lens, min(team, C::kTeams - 1))
+                              : find_share<C>(a, lens, reinterpret_cast<int *>(shared + C::offScan), min(team, C::kTeams - 1));
     const int count = sh.u1 - sh.u0;
     Place<C> at{};
-    if (count > 0) {
+    if (count > 0 || kClusters) {
         const int len = length_of(a, lens, sh.b), end = units_of<C::kUnitKeys>(len), in = sh.u0 - sh.before;
         at.set(sh.b, in / end, in % end, len);
     }
 
     if (loads) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
-        if (team >= C::kTeams || count == 0) return;
+        if (team < C::kTeams && count > 0) {
         // ------------------------------------------------------------------ loads: a lane per block, four units to a batch of table entries
-        constexpr int kBatch = 32 / C::kBlocks;
-        const uint8_t *pool = after_wait(a.pool);
-        const int mine = lane / C::kBlocks, block = lane % C::kBlocks;
-        ArmCounts<S> armed;
-        int base = at.t, nb, nh, nlen, stage = 0, round = 0;
-        long long cur = block_offset<D, true, C>(a, table, at.b, at.h, base + mine, block), nxt;
-        auto fetch_next = [&] {      // the batch behind the current one
-            nb = at.b; nh = at.h; nlen = at.len;
-            int nt = base + kBatch;
-            if (nt >= at.end) {
-                nt = 0;
-                if (++nh == a.Hkv) { nh = 0; nlen = length_of(a, lens, ++nb); }
+            constexpr int kBatch = 32 / C::kBlocks;
+            const uint8_t *pool = after_wait(a.pool);
+            const int mine = lane / C::kBlocks, block = lane % C::kBlocks;
+            ArmCounts<S> armed;
+            int base = at.t, nb, nh, nlen, stage = 0, round = 0;
+            long long cur = block_offset<D, true, C>(a, table, at.b, at.h, base + mine, block), nxt;
+            auto fetch_next = [&] {      // the batch behind the current one
+                nb = at.b; nh = at.h; nlen = at.len;
+                int nt = base + kBatch;
+                if (nt >= at.end) {
+                    nt = 0;
+                    if (++nh == a.Hkv) { nh = 0; nlen = length_of(a, lens, ++nb); }
+                }
+                nxt = block_offset<D, true, C>(a, table, nb, nh, nt + mine, block);
+            };
+            fetch_next();
+            for (int i = 0; i < count; ++i) {
+                bool ok = round == 0 || mbar_wait(empty + stage, (round - 1) & 1, abortp, a.status, PERR_EMPTY);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const bool valid = mine == at.t - base && cur >= 0 && at.t * C::kUnitKeys + 16 * block < at.len;
+                const uint32_t who = __ballot_sync(0xffffffffu, valid);
+                if (lane == 0) {
+                    live[stage] = who >> ((at.t - base) * C::kBlocks);
+                    mbar_arm(full, stage, (uint32_t)(__popc(who) * C::kBlock), armed);
+                }
+                __syncwarp();
+                if (valid) bulk_load_1d(smem + stage * kUnit + block * C::kBlock, pool + cur, C::kBlock, full + stage);
+                if (++stage == S) { stage = 0; ++round; }
+                ++at.t;
+                const bool over = at.t == at.end;
+                if (over || at.t == base + kBatch) {
+                    if (over) at.set(nb, nh, 0, nlen);
+                    base = at.t;
+                    cur = nxt;
+                    fetch_next();
+                }
             }
-            nxt = block_offset<D, true, C>(a, table, nb, nh, nt + mine, block);
-        };
-        fetch_next();
-        for (int i = 0; i < count; ++i) {
-            bool ok = round == 0 || mbar_wait(empty + stage, (round - 1) & 1, abortp, a.status, PERR_EMPTY);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            const bool valid = mine == at.t - base && cur >= 0 && at.t * C::kUnitKeys + 16 * block < at.len;
-            const uint32_t who = __ballot_sync(0xffffffffu, valid);
-            if (lane == 0) {
-                live[stage] = who >> ((at.t - base) * C::kBlocks);
-                mbar_arm(full, stage, (uint32_t)(__popc(who) * C::kBlock), armed);
-            }
-            __syncwarp();
-            if (valid) bulk_load_1d(smem + stage * kUnit + block * C::kBlock, pool + cur, C::kBlock, full + stage);
-            if (++stage == S) { stage = 0; ++round; }
-            ++at.t;
-            const bool over = at.t == at.end;
-            if (over || at.t == base + kBatch) {
-                if (over) at.set(nb, nh, 0, nlen);
-                base = at.t;
-                cur = nxt;
-                fetch_next();
-            }
+            if (lane == 0) mbar_drain(full, armed);      // copies still on their way land before the CTA leaves (bounded)
         }
-        if (lane == 0) mbar_drain(full, armed);      // copies still on their way land before the CTA leaves (bounded)
+        __syncwarp();
+        if constexpr (kClusters) {
+            cluster_sync_all();
+            cluster_sync_all();
+        }
         return;
     }
 
@@ -640,7 +718,7 @@ __global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ
     const uint32_t ring = smem_u32(smem);
     int stage = 0, parity = 0;
     bool ok = true;
-    walk<D, true, NQ>(a, sh, at, after_wait(a.q), lens, smem, team, [&](HeadState<D, true, NQ> &s, const Place<C> &use) {
+    walk<D, true, NQ, kClusters>(a, sh, at, after_wait(a.q), lens, smem, team, [&](HeadState<D, true, NQ> &s, const Place<C> &use) {
         if (ok && !mbar_wait(full + stage, parity, abortp, a.status, PERR_FULL)) ok = false;
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) return;
@@ -650,9 +728,16 @@ __global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ
         if (lane == 0) mbar_arrive(empty + stage);
         if (++stage == S) { stage = 0; parity ^= 1; }
     });
+    if constexpr (kClusters) {
+        __syncwarp();
+        cluster_sync_all();
+        combine<D, true, NQ>(a, shared, (int)cluster_ctarank() * (128 * C::kTeams) + tid, a.cl * 128 * C::kTeams);
+        __syncwarp();
+        cluster_sync_all();      // nobody leaves while another CTA may still read its shared memory
+    }
 }
 
-template <int D, int NQ>
+template <int D, int NQ, bool kClusters>
 __global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, NQ>::kCtas)) paged_decode16_kernel(const PagedArgs a)
 {
     using C = Cfg<D, false, NQ>;
@@ -663,9 +748,9 @@ __global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, 
     grid_launch_dependents();
     const int *lens = after_wait(a.lens), *table = after_wait(a.table);
     const uint8_t *pool = after_wait(a.pool);
-    const Share sh = find_share<C>(a, lens, reinterpret_cast<int *>(smem + C::offScan), 0);
+    const Share sh = kClusters ? cluster_share<C>(a, lens, 0) : find_share<C>(a, lens, reinterpret_cast<int *>(smem + C::offScan), 0);
     const int count = sh.u1 - sh.u0;
-    if (count == 0) {
+    if (count == 0 && !kClusters) {
         if (tid == 0) a.info[sh.c] = make_int2(-1, 0);
         return;
     }
@@ -728,7 +813,7 @@ __global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, 
     // ---- use
     const float margin = kRescale / a.scale_log2;
     int get = 0;      // stage of this step
-    walk<D, false, NQ>(a, sh, start, after_wait(a.q), lens, smem, 0, [&](HeadState<D, false, NQ> &s, const Place<C> &use) {
+    walk<D, false, NQ, kClusters>(a, sh, start, after_wait(a.q), lens, smem, 0, [&](HeadState<D, false, NQ> &s, const Place<C> &use) {
         cp_wait<S - 2>();
         __syncwarp();
         const uint32_t st = ring + get * C::kBlock, here = live >> get & 1;
@@ -736,7 +821,15 @@ __global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, 
         get = get == S - 1 ? 0 : get + 1;
         if (here) s.step(st, here, use.len - (use.t * C::kUnitKeys + 16 * warp), a.scale_log2, margin, lane);
     });
-    cp_wait<0>();
+    if constexpr (kClusters) {
+        __syncwarp();
+        cluster_sync_all();
+        combine<D, false, NQ>(a, smem, (int)cluster_ctarank() * 128 + tid, a.cl * 128);
+        __syncwarp();
+        cluster_sync_all();      // nobody leaves while another CTA may still read its shared memory
+    } else {
+        cp_wait<0>();
+    }
 }
 
 // Heads that lie in several shares: block (c, query) joins the partial results of the head that begins in share c and goes on, its 128 threads in
@@ -820,11 +913,17 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
                    cudaStream_t st)
 {
     using C = Cfg<D, kInt4, NQ>;
-    constexpr auto kernel = [] { if constexpr (kInt4) return paged_decode4_kernel<D, NQ>; else return paged_decode16_kernel<D, NQ>; }();
-    const cudaError_t e = allow_smem<kernel>(C::kTotal);
-    if (e != cudaSuccess) return e;
+    constexpr auto kernel = [] { if constexpr (kInt4) return paged_decode4_kernel<D, NQ, false>; else return paged_decode16_kernel<D, NQ, false>; }();
+    constexpr auto clusters = [] { if constexpr (kInt4) return paged_decode4_kernel<D, NQ, true>; else return paged_decode16_kernel<D, NQ, true>; }();
     const int G = p.H / p.pool.Hkv, sms = device_info().sms, shares = shares_for(p, C::kShares, C::kUnitKeys), most = 4 * sms;
-    const int ctas = std::min(shares, C::kCtas * sms);
+    const int heads = p.B * p.pool.Hkv, slots = C::kCtas * sms, units = (int)(((long long)p.max_pages * p.pool.page + C::kUnitKeys - 1) / C::kUnitKeys);
+    // A cluster for each head, and no merge kernel, while all of them fit at once (clusters of 4 and 8 leave SMs of a GPC over) and a CTA does not stream
+    // more than 192 KB beyond an equal share of what the tables have room for, about what the merge kernel costs.
+    int cl = 0;
+    for (int c = 1; c <= 8 && (long long)heads * c * 100 <= slots * (c == 8 ? 85LL : c == 4 ? 90LL : 100LL); c *= 2) cl = c;
+    const long long mine = cl ? (units + cl - 1) / cl : 0, equal = ((long long)units * heads + slots - 1) / slots;
+    if (cl && (mine - equal) * C::kBlocks * C::kBlock > 192 * 1024) cl = 0;
+    const int ctas = cl ? heads * cl : std::min(shares, slots);
     PagedArgs a{};
     a.q = (const __nv_bfloat16 *)q; a.pool = (const uint8_t *)pool; a.table = table; a.lens = lens;
     a.out = (__nv_bfloat16 *)out; a.lse = lse;
@@ -837,12 +936,17 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     a.cap = (int)((long long)p.max_pages * p.pool.page);
     a.by_page = FastDiv((uint32_t)p.pool.page);
     a.status = device_status_ptr();
+    a.cl = cl;
     a.scale_log2 = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
     a.sign2 = p.scale == 0.f ? 0u : p.scale > 0.f ? 0x3f803f80u : 0xbf80bf80u;
+    const cudaError_t e = cl ? allow_smem<clusters>(C::kTotal) : allow_smem<kernel>(C::kTotal);
+    if (e != cudaSuccess) return e;
     {
         LaunchScope scope(MOA_KERNEL_OTHER, st);
-        const cudaError_t le = launch_dependent(kernel, dim3((unsigned)ctas), dim3(C::kThreads), (size_t)C::kTotal, st, a);
-        if (le != cudaSuccess) return le;
+        const dim3 grid((unsigned)ctas), block(C::kThreads);
+        const cudaError_t le = cl ? launch_cluster(clusters, (unsigned)cl, grid, block, (size_t)C::kTotal, st, a)
+                                  : launch_dependent(kernel, grid, block, (size_t)C::kTotal, st, a);
+        if (le != cudaSuccess || cl) return le;
     }
     LaunchScope scope(MOA_KERNEL_OTHER, st);
     return launch_dependent(paged_merge_kernel<D>, dim3((unsigned)std::min(shares, ctas * C::kTeams), (unsigned)G), dim3(128), (size_t)0, st, (const int2 *)a.info, (const float *)a.part_o,
