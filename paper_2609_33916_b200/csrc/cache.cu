@@ -17,7 +17,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 256, kTokens = 4, kUnroll = 2;
+constexpr int kThreads = 256, kTokens = 4, kUnroll = 2, kResident = 4;
 using Piece = Chunk<__nv_bfloat16, 8>;
 
 // x / d where x may pass 31 bits
@@ -33,7 +33,7 @@ struct AppendArgs {
     RopeStride sq, sk, sv, so;
     long long page_stride, keys;     // keys: of the whole pool
     int T, H, Hkv, page, d_rot, tt;
-    FastDiv by_heads, by_kv, by_page;      // H, H_kv, page
+    FastDiv by_heads, by_kv, by_page, by_freqs;      // H, H_kv, page, d_rot / 2
     float factor;
 };
 
@@ -178,7 +178,7 @@ __device__ __forceinline__ void turn_key(Piece &x, Piece &y, const float (&c)[8]
 
 // Blocks of a tile of tokens: gridDim.y == 1: one with all its rows; else the last one keys and values, the others the queries
 template <int D, bool kInt4, bool kPairs>
-__global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const AppendArgs a)
+__global__ void __launch_bounds__(kThreads, kResident) kv_append_kernel(const AppendArgs a)
 {
     constexpr int kLanes = D / 16, kPer = kThreads / kLanes;
     __shared__ float4 angles[kTokens * D / 4];
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const AppendArgs
     int row = qpart * (kPer * kUnroll) + r0;
     load_q(row);
     for (int i = tid; i < nt * freqs; i += kThreads) {
-        const int t = i / freqs, f = i - t * freqs;
+        const int t = (int)a.by_freqs.div((uint32_t)i), f = i - t * freqs;
         float2 cs = position_angle(pos[t0 + t], inv_freq[f]);
         cs.x *= a.factor;
         cs.y *= a.factor;
@@ -311,34 +311,57 @@ struct GatherArgs {
     FastDiv by_page;
 };
 
-__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&f)[8])
+// Four codes, nibbles 0..3 of the low half of h in the order of the elements, or eight of K's word, as pairs at the low ends of the halves of a word
+__device__ __forceinline__ void spread(uint32_t h, uint32_t (&pair)[2])
+{
+    pair[0] = (h | h << 12) & 0x000f000fu;
+    pair[1] = (h >> 8 | h << 4) & 0x000f000fu;
+}
+// Pairs of codes to values: 128 + c as bf16, minus 136, times the scale: exact until the product's one rounding
+__device__ __forceinline__ void store_codes(__nv_bfloat16 *p, const uint32_t (&pair)[4], uint32_t scale)
+{
+    uint32_t w[4];
+    const uint32_t s2 = scale | scale << 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t x = pair[i] | 0x43004300u;
+        asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(w[i]) : "r"(x), "r"(0xc308c308u));
+        asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(w[i]) : "r"(s2));
+    }
+    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store_codes(float *p, const uint32_t (&pair)[4], uint32_t scale)
+{
+    const float s = __uint_as_float(scale << 16);
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = s * (float)((int)(pair[i] & 15u) - 8);
+        f[2 * i + 1] = s * (float)((int)(pair[i] >> 16) - 8);
+    }
+    reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+}
+__device__ __forceinline__ void store16(__nv_bfloat16 *p, const uint4 &w) { *reinterpret_cast<uint4 *>(p) = w; }
+__device__ __forceinline__ void store16(float *p, const uint4 &w)
 {
     Piece x;
-    x.pack(f);
-    *reinterpret_cast<uint4 *>(p) = x.w;
-}
-__device__ __forceinline__ void store8(float *p, const float (&f)[8])
-{
+    float f[8];
+    x.w = w;
+    x.unpack(f);
     reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
     reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
 }
 
 // A row of a head is d / 8 lanes with 8 elements each.  A block takes 16 tokens (the codes of 16 neighbouring values share sectors) and kGatherRows
-// of their 2 H_kv rows: first their slots, then all codes and scales of a lane are on their way, then the results.
+// heads of K or of V: first the slots, then all codes and scales of a lane are on their way, then the results.
 constexpr int kGatherRows = 4, kGatherTokens = 16;
 
-template <typename T, int D, bool kInt4>
-__global__ void __launch_bounds__(kGatherTokens * D / 8) kv_gather_kernel(const GatherArgs a)
+template <typename T, int D, bool kInt4, bool kV>
+__device__ __forceinline__ void gather_rows(const GatherArgs &a, const uint8_t *pool, long long at, int t, int h0)
 {
-    constexpr int kLanes = D / 8;
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const uint8_t *pool = after_wait(a.pool);
-    const long long *slots = after_wait(a.slot);
-    const int c = threadIdx.x % kLanes, y = c / 4, t8 = c % 4, t = blockIdx.x * kGatherTokens + threadIdx.x / kLanes, first = blockIdx.y * kGatherRows;
     using L = Block4<D>;
-    if (t >= a.T) return;
-    const long long at = slots[t];
+    const int c = threadIdx.x % (D / 8), y = c / 4, t8 = c % 4;
     const bool there = at >= 0 && at < a.keys;
     const long long pg = there ? divide(at, a.by_page) : 0;
     const int key = there ? (int)(at - pg * a.page) : 0, r = key % kBlockKeys;
@@ -347,39 +370,56 @@ __global__ void __launch_bounds__(kGatherTokens * D / 8) kv_gather_kernel(const 
 #pragma unroll
     for (int u = 0; u < kGatherRows; ++u) {
         raw[u] = make_uint4(0u, 0u, 0u, 0u);
-        const int v = first + u >= a.Hkv, h = first + u - v * a.Hkv;
-        if (!there || h >= a.Hkv) continue;
+        if (!there || h0 + u >= a.Hkv) continue;
         if constexpr (!kInt4) {
-            raw[u] = *reinterpret_cast<const uint4 *>(page + row16(a.page, D, h, v, key) + 16 * c);
+            raw[u] = *reinterpret_cast<const uint4 *>(page + row16(a.page, D, h0 + u, kV, key) + 16 * c);
         } else {
-            const uint8_t *blk = page + block4<D>(a.page, h, key / kBlockKeys);
-            raw[u].x = *reinterpret_cast<const uint32_t *>(blk + (v ? L::v_word(r, 2 * t8, y / 2) : L::k_word(r, t8, y)));
-            if (v) raw[u].y = *reinterpret_cast<const uint32_t *>(blk + L::v_word(r, 2 * t8 + 1, y / 2));
-            raw[u].z = *reinterpret_cast<const uint16_t *>(blk + (v ? L::v_scale(r, y) : L::k_scale(r, y)));
+            const uint8_t *blk = page + block4<D>(a.page, h0 + u, key / kBlockKeys);
+            raw[u].x = *reinterpret_cast<const uint32_t *>(blk + (kV ? L::v_word(r, 2 * t8, y / 2) : L::k_word(r, t8, y)));
+            if (kV) raw[u].y = *reinterpret_cast<const uint32_t *>(blk + L::v_word(r, 2 * t8 + 1, y / 2));
+            raw[u].z = *reinterpret_cast<const uint16_t *>(blk + (kV ? L::v_scale(r, y) : L::k_scale(r, y)));
         }
     }
+    T *dst = kV ? (T *)a.v + a.sv.at(t, h0) : (T *)a.k + a.sk.at(t, h0);
+    const int step = kV ? a.sv.head : a.sk.head;
 #pragma unroll
     for (int u = 0; u < kGatherRows; ++u) {
-        const int v = first + u >= a.Hkv, h = first + u - v * a.Hkv;
-        if (h >= a.Hkv) break;
-        float f[8];
+        if (h0 + u >= a.Hkv) break;
+        T *p = dst + (long long)u * step + 8 * c;
         if constexpr (!kInt4) {
-            Piece x;
-            x.w = raw[u];
-            x.unpack(f);
+            store16(p, raw[u]);
         } else {
-            // (the places of a group's elements: in order for V, the even ones and then the odd ones for K; no such slot: scale 0)
-            const int sh = 16 * (y % 2);
-            const uint32_t code = v ? ((raw[u].x >> sh) & 0xffffu) | ((raw[u].y >> sh) << 16) : raw[u].x;
-            const float s = __uint_as_float(raw[u].z << 16);
+            uint32_t pair[4];      // (no such slot: scale 0)
+            if (kV) {
+                const int sh = 16 * (y % 2);
+                uint32_t lo[2], hi[2];
+                spread((raw[u].x >> sh) & 0xffffu, lo);
+                spread((raw[u].y >> sh) & 0xffffu, hi);
+                pair[0] = lo[0]; pair[1] = lo[1]; pair[2] = hi[0]; pair[3] = hi[1];
+            } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t n = v ? code >> (4 * i) : code >> (4 * (4 * (i % 2) + i / 2));
-                f[i] = s * (float)((int)(n & 15u) - 8);
+                for (int i = 0; i < 4; ++i) pair[i] = raw[u].x >> (4 * i) & 0x000f000fu;
             }
+            if (!there) pair[0] = pair[1] = pair[2] = pair[3] = 0x00080008u;      // (+0)
+            store_codes(p, pair, raw[u].z);
         }
-        store8((v ? (T *)a.v + a.sv.at(t, h) : (T *)a.k + a.sk.at(t, h)) + 8 * c, f);
     }
+}
+
+template <typename T, int D, bool kInt4>
+__global__ void __launch_bounds__(kGatherTokens * D / 8) kv_gather_kernel(const GatherArgs a)
+{
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const uint8_t *pool = after_wait(a.pool);
+    const long long *slots = after_wait(a.slot);
+    const int t = blockIdx.x * kGatherTokens + threadIdx.x / (D / 8), parts = (int)gridDim.y / 2, part = (int)blockIdx.y;
+    if (t >= a.T) return;
+    const long long at = slots[t];
+    if (part < parts)
+        gather_rows<T, D, kInt4, false>(a, pool, at, t, part * kGatherRows);
+    else
+        gather_rows<T, D, kInt4, true>(a, pool, at, t, (part - parts) * kGatherRows);
 }
 
 template <int D, bool kInt4>
@@ -393,7 +433,7 @@ cudaError_t launch_append(const AppendArgs &a, bool pairs, dim3 grid, cudaStream
 template <typename T>
 cudaError_t launch_gather(const GatherArgs &a, int d, int int4, cudaStream_t st)
 {
-    const dim3 grid((unsigned)((a.T + kGatherTokens - 1) / kGatherTokens), (unsigned)((2 * a.Hkv + kGatherRows - 1) / kGatherRows)), block(kGatherTokens * d / 8);
+    const dim3 grid((unsigned)((a.T + kGatherTokens - 1) / kGatherTokens), (unsigned)(2 * ((a.Hkv + kGatherRows - 1) / kGatherRows))), block(kGatherTokens * d / 8);
     LaunchScope scope(MOA_KERNEL_OTHER, st);
     if (d == 64)
         return int4 ? launch_dependent(kv_gather_kernel<T, 64, true>, grid, block, (size_t)0, st, a)
@@ -419,8 +459,8 @@ cudaError_t kv_append(const AppendProblem &p, const void *q, const void *k, cons
     a.by_page = FastDiv((uint32_t)p.pool.page);
     a.factor = p.factor;
     const int per = kThreads / (p.pool.d / 16), sms = device_info().sms;
-    a.tt = kTokens;
-    while (a.tt > 1 && (p.T + a.tt - 1) / a.tt < 4 * sms) a.tt /= 2;
+    a.by_freqs = FastDiv((uint32_t)(p.d_rot > 0 ? p.d_rot / 2 : 1));
+    a.tt = tokens_per_block(p.T, kTokens, kResident * sms);
     const int blocks = (p.T + a.tt - 1) / a.tt;
     // few tokens: keys and values in a block of their own, the queries in as many more as fill the SMs
     int split = 1;

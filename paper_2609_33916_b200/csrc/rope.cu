@@ -13,7 +13,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 256, kTokens = 4, kUnroll = 2;
+constexpr int kThreads = 256, kTokens = 4, kUnroll = 2, kResident = 5;
 
 struct RopeArgs {
     const int *pos;
@@ -23,12 +23,12 @@ struct RopeArgs {
     RopeStride sq, sk, so, sko;
     int T, H, d, d_rot, tt;      // tt: tokens per block
     int lanes, np;               // lanes per row; those of them that rotate
-    FastDiv rows, by_lanes;      // heads of q and k
+    FastDiv rows, by_lanes, by_freqs;      // heads of q and k, lanes, d_rot / 2
     float factor, sign;
 };
 
 template <typename T, int V, bool kPairs>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a)
+__global__ void __launch_bounds__(kThreads, kResident) rope_kernel(const RopeArgs a)
 {
     __shared__ float4 angles[kTokens * 64];      // (256 elements: 128 angles of 8 bytes per token)
     const int tid = threadIdx.x, t0 = blockIdx.x * a.tt, nt = min(a.tt, a.T - t0), freqs = a.d_rot / 2;
@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a)
     const int *pos = after_wait(a.pos);
     const float *inv_freq = after_wait(a.inv_freq);
     for (int i = tid; i < nt * freqs; i += kThreads) {
-        const int t = i / freqs, f = i - t * freqs;
+        const int t = (int)a.by_freqs.div((uint32_t)i), f = i - t * freqs;
         float2 cs = position_angle(pos[t0 + t], inv_freq[f]);
         cs.x *= a.factor;
         cs.y *= a.factor * a.sign;
@@ -110,8 +110,8 @@ cudaError_t launch(const RopeProblem &p, const int *pos, const float *inv_freq, 
     a.factor = p.factor;
     a.sign = p.backward ? -1.f : 1.f;
     // a few tokens: one to a block, and its rows over several
-    a.tt = kTokens;
-    while (a.tt > 1 && (p.T + a.tt - 1) / a.tt < 4 * sms) a.tt /= 2;
+    a.by_freqs = FastDiv((uint32_t)(p.d_rot / 2));
+    a.tt = tokens_per_block(p.T, kTokens, kResident * sms);
     const int blocks = (p.T + a.tt - 1) / a.tt, passes = (a.tt * rows + per * kUnroll - 1) / (per * kUnroll);
     int split = 1;
     while (split < passes && blocks * split < 2 * sms) ++split;
