@@ -94,15 +94,15 @@ __device__ __forceinline__ void quantise16(const Piece &lo, const Piece &hi, uin
     if (plain) {
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
+            // Adding 1.5 * 2^23 + 8 leaves the code, rounded half to even, in the low bits (|x / s| <= 7 (1 + 2^-8): at most 7); the words of all eight,
+            // each 16 times the next, add up to the codes and a constant.
             uint32_t c = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 7; i >= 0; --i) {
                 const float v = x[w][i], q0 = v * inv, q1 = fmaf(fmaf(-q0, s, v), inv, q0);
-                // adding 1.5 * 2^23 leaves the integer, rounded half to even, in the low bits
-                const int n = (int)(__float_as_uint(q1 + 12582912.f) - 0x4b400000u);
-                c |= (uint32_t)(min(max(n, -7), 7) + 8) << (4 * i);
+                c = c * 16u + __float_as_uint(q1 + 12582920.f);
             }
-            code[w] = c;
+            code[w] = c - 0x4b400000u * 0x11111111u;
         }
     }
     scale = (uint16_t)(__float_as_uint(s) >> 16);
