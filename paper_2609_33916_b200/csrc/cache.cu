@@ -17,7 +17,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 256, kTokens = 4, kUnroll = 2, kResident = 4;
+constexpr int kThreads = 128, kTokens = 2, kUnroll = 2, kResident = 8;
 using Piece = Chunk<__nv_bfloat16, 8>;
 
 // x / d where x may pass 31 bits
