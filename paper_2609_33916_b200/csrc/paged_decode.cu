@@ -15,9 +15,10 @@
 // ring of its own (cp.async with the swizzle that ldmatrix wants; no barrier among warps), the entries of its next 32 steps in its lanes.
 //
 // Work split: a unit is 64 (bf16) or 128 keys of a K/V head, a step of each warp of a CTA.  All units of all sequences, in the order sequence, head, key, are cut into
-// equal shares, one per resident CTA, on the device (the host does not know the lengths): every CTA adds up the lengths and finds its
-// share.  A head that lies in one share is written at once; the others leave partial results (at most two per CTA) and a merge kernel, set up meanwhile,
-// joins them: CTA c tells it which head begins in its share and goes on, and where that ends.
+// equal shares, one per resident team, on the device (the host does not know the lengths): every CTA adds up the lengths and finds its
+// teams' shares.  A head that lies in one share is written at once; the teams of the others leave partial results (at most two each), and the last of
+// them to come joins them, told by a counter that a one-block kernel in front has cleared; the streaming starts without waiting for that.
+// Where there are few heads, a cluster takes each and joins its teams through distributed shared memory.
 #include "cache_layout.cuh"
 #include "ptx.cuh"
 #include <algorithm>
@@ -38,7 +39,7 @@ struct PagedArgs {
     const int *table, *lens;
     __nv_bfloat16 *out;
     float *lse, *part_o, *part_ml;
-    int2 *info;                 // of a share: the head that begins in it and goes on (-1: none), the share that ends it
+    unsigned int *counters;     // of a share: how many of those that hold the head that begins in it and goes on have left their part
     RopeStride sq;
     long long table_stride, page_stride;
     int B, Hkv, G, pages, page, cap;      // cap: keys that a row of the table has room for
@@ -64,7 +65,8 @@ struct Cfg {
     static constexpr int offMerge = kStages * kBlocks * kBlock;
     static constexpr int offMl = offMerge + kWarps * 8 * kLd * 4;                      // [warps][8] (maximum, sum)
     static constexpr int offBar = offMl + kWarps * 8 * 8;                              // full, empty [stages], then [stages] words: blocks that hold keys
-    static constexpr int kTeam = (offBar + kStages * 20 + 4 + 127) / 128 * 128;
+    static constexpr int offFlag = offBar + kStages * 20 + 4;
+    static constexpr int kTeam = (offFlag + 4 + 127) / 128 * 128;
     static constexpr int offScan = kTeams * kTeam;                                     // of the CTA: 16 words of sums, two for each team
     static constexpr int kTotal = offScan + 128;
     static constexpr int kNO = D / 16;                                                 // tiles of O^T
@@ -549,10 +551,66 @@ __device__ __forceinline__ void join(const PagedArgs &a, const HeadState<D, kInt
     }
 }
 
+// The share that holds unit u
+__device__ __forceinline__ int share_of(const Share &sh, int u)
+{
+    int c = (int)((long long)u * sh.shares / sh.units);
+    while (first_unit(sh.units, c + 1, sh.shares) <= u) ++c;
+    return c;
+}
+
+// A head that lies in several shares, ca to cb: the team that leaves its part last joins them all (nobody waits for anyone).
+template <int D, class C>
+__device__ __forceinline__ void last_joins(const PagedArgs &a, int team, int head, int ca, int cb, unsigned int *flag)
+{
+    constexpr int kJoin = 32 * kWarps, kBatch = 4;
+    const int tid = threadIdx.x % kJoin;
+    __threadfence();                            // (this thread's part, before the count)
+    named_barrier(1 + team, kJoin);
+    if (tid == 0) *flag = atomicAdd(a.counters + ca, 1u);
+    named_barrier(1 + team, kJoin);
+    if (*flag != (unsigned)(cb - ca)) return;
+    __threadfence();
+    for (int idx = tid; idx < a.G * (D / 4); idx += kJoin) {
+        const int g = idx / (D / 4), c = 4 * (idx % (D / 4));
+        float mt = -INFINITY, ls = 0.f;
+        float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k0 = ca; k0 <= cb; k0 += kBatch) {
+            float2 ml[kBatch];
+            float4 v[kBatch];
+            float mn = mt;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const size_t at = (size_t)(2 * (k0 + u) + (k0 + u == ca ? 1 : 0)) * a.G + g;
+                const bool there = k0 + u <= cb;
+                ml[u] = there ? __ldcg(reinterpret_cast<const float2 *>(a.part_ml + at * 2)) : make_float2(-INFINITY, 0.f);
+                v[u] = there ? __ldcg(reinterpret_cast<const float4 *>(a.part_o + at * D + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, ml[u].x);
+            const float ref = mn == -INFINITY ? 0.f : mn, b = ex2(mt - ref);
+            mt = mn;
+            ls *= b;
+            ot.x *= b; ot.y *= b; ot.z *= b; ot.w *= b;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const float f = ex2(ml[u].x - ref);
+                ls = fmaf(ml[u].y, f, ls);
+                ot.x = fmaf(v[u].x, f, ot.x); ot.y = fmaf(v[u].y, f, ot.y); ot.z = fmaf(v[u].z, f, ot.z); ot.w = fmaf(v[u].w, f, ot.w);
+            }
+        }
+        const size_t at = (size_t)head * a.G + g;
+        const float inv = ls == 0.f ? 0.f : 1.f / ls;
+        *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
+        if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + log2f(ls)) * kLn2;
+    }
+}
+
 // The segments of a share in turn: `next` makes a step of this warp with the head's state
 template <int D, bool kInt4, int NQ, bool kClusters, class Next>
 __device__ __forceinline__ void walk(const PagedArgs &a, const Share &sh, Place<Cfg<D, kInt4, NQ>> use, const __nv_bfloat16 *q, const int *lens, uint8_t *smem, int team, Next next)
 {
+    using C = Cfg<D, kInt4, NQ>;
     const int count = sh.u1 - sh.u0, lane = threadIdx.x % 32;
     int done = 0;
     HeadState<D, kInt4, NQ> s;
@@ -563,19 +621,17 @@ __device__ __forceinline__ void walk(const PagedArgs &a, const Share &sh, Place<
         join<D, kInt4, NQ, true>(a, s, smem, team, 0, false, 0);
         return;
     }
-    int2 told = make_int2(-1, 0);
     while (done < count) {
         const int first = use.t, steps = min(use.end - use.t, count - done), head = use.b * a.Hkv + use.h;
         s.begin(a, q, use.b, use.h, lane);
         for (int i = 0; i < steps; ++i, ++done, ++use.t) next(s, use);
         const bool whole = first == 0 && use.t == use.end;
         join<D, kInt4, NQ, false>(a, s, smem, team, head, whole, 2 * sh.c + (first == 0 ? 1 : 0));
-        if (!whole && first == 0) {
-            // the head's last unit, and whose share that is in
-            const int last = sh.u0 + done - use.t + use.end - 1;
-            int c = (int)((long long)last * sh.shares / sh.units);
-            while (first_unit(sh.units, c + 1, sh.shares) <= last) ++c;
-            told = make_int2(head, c);
+        if (!whole) {
+            // the head's first and last unit, and whose shares those are in
+            const int next_unit = sh.u0 + done;
+            last_joins<D, C>(a, team, head, first == 0 ? sh.c : share_of(sh, next_unit - use.t),
+                             use.t == use.end ? sh.c : share_of(sh, next_unit - use.t + use.end - 1), reinterpret_cast<unsigned int *>(smem + C::offFlag));
         }
         if (use.t == use.end) {
             int b = use.b, h = use.h + 1;
@@ -583,7 +639,6 @@ __device__ __forceinline__ void walk(const PagedArgs &a, const Share &sh, Place<
             use.set(b, h, 0, b == use.b ? use.len : length_of(a, lens, b));
         }
     }
-    if (threadIdx.x % (32 * kWarps) == 0) a.info[sh.c] = told;
 }
 
 // A cluster's teams joined through distributed shared memory.  Each CTA makes a contiguous part of the head's elements, four of them in eight lanes: lane k
@@ -659,8 +714,11 @@ __global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ
         *abortp = 0;
         fence_mbar_init();
     }
-    grid_dependency_wait();
-    grid_launch_dependents();
+    // (without clusters the kernel in front is the one that clears the counters: only who uses them waits for it)
+    if constexpr (kClusters) {
+        grid_dependency_wait();
+        grid_launch_dependents();
+    }
     const int *lens = after_wait(a.lens), *table = after_wait(a.table);
     if constexpr (kClusters) __syncthreads();                    // (else the barriers of find_share are those of the set-up too)
     const Share sh = kClusters ? cluster_share<C>(a, lens, min(team, C::kTeams - 1))
@@ -727,6 +785,10 @@ __global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ
     // ---------------------------------------------------------------------- use
     const float scale = a.scale_log2 * exp2i(-kCodeExp1 - kLift), margin = kRescale / scale;
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kUseRegs));
+    if constexpr (!kClusters) {
+        grid_dependency_wait();
+        grid_launch_dependents();
+    }
     const uint32_t ring = smem_u32(smem);
     int stage = 0, parity = 0;
     bool ok = true;
@@ -756,16 +818,16 @@ __global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, 
     constexpr int S = C::kStages;
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
-    grid_dependency_wait();
-    grid_launch_dependents();
+    // (without clusters the kernel in front is the one that clears the counters)
+    if constexpr (kClusters) {
+        grid_dependency_wait();
+        grid_launch_dependents();
+    }
     const int *lens = after_wait(a.lens), *table = after_wait(a.table);
     const uint8_t *pool = after_wait(a.pool);
     const Share sh = kClusters ? cluster_share<C>(a, lens, 0) : find_share<C>(a, lens, reinterpret_cast<int *>(smem + C::offScan), 0);
     const int count = sh.u1 - sh.u0;
-    if (count == 0 && !kClusters) {
-        if (tid == 0) a.info[sh.c] = make_int2(-1, 0);
-        return;
-    }
+    if (count == 0 && !kClusters) return;
     Place<C> ask;
     {
         const int len = length_of(a, lens, sh.b), end = units_of<C::kUnitKeys>(len), in = sh.u0 - sh.before;
@@ -823,6 +885,10 @@ __global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, 
     for (int i = 0; i < S - 1; ++i) request(i);
 
     // ---- use
+    if constexpr (!kClusters) {
+        grid_dependency_wait();
+        grid_launch_dependents();
+    }
     const float margin = kRescale / a.scale_log2;
     int get = 0;      // stage of this step
     walk<D, false, NQ, kClusters>(a, sh, start, after_wait(a.q), lens, smem, 0, [&](HeadState<D, false, NQ> &s, const Place<C> &use) {
@@ -844,75 +910,6 @@ __global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, 
     }
 }
 
-// Heads that lie in several shares: block (c, query) joins the partial results of the head that begins in share c and goes on, its 128 threads in
-// stripes of D / 4 over the shares.
-template <int D>
-__global__ void __launch_bounds__(128)
-paged_merge_kernel(const int2 *__restrict__ info, const float *__restrict__ part_o, const float *__restrict__ part_ml, __nv_bfloat16 *__restrict__ out,
-                   float *__restrict__ lse, int G)
-{
-    constexpr int kLanes = D / 4, kStripes = 128 / kLanes, kBatch = 8;
-    __shared__ float4 so[kStripes][kLanes];
-    __shared__ float2 sml[kStripes];
-    const int ca = (int)blockIdx.x, g = (int)blockIdx.y;
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const int2 told = after_wait(info)[ca];
-    const int head = told.x, cb = told.y;
-    if (head < 0) return;
-    part_o = after_wait(part_o);
-    part_ml = after_wait(part_ml);
-    const int stripe = (int)threadIdx.x / kLanes, lane = (int)threadIdx.x % kLanes, c = 4 * lane;
-    float mt = -INFINITY, ls = 0.f;
-    float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = ca + stripe; k0 <= cb; k0 += kStripes * kBatch) {
-        float2 ml[kBatch];
-        float4 v[kBatch];
-        float mn = mt;
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const int k = k0 + u * kStripes;
-            const size_t at = (size_t)(2 * k + (k == ca ? 1 : 0)) * G + g;
-            const bool there = k <= cb;
-            ml[u] = there ? *reinterpret_cast<const float2 *>(part_ml + at * 2) : make_float2(-INFINITY, 0.f);
-            v[u] = there ? *reinterpret_cast<const float4 *>(part_o + at * D + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, ml[u].x);
-        const float ref = mn == -INFINITY ? 0.f : mn, b = ex2(mt - ref);
-        mt = mn;
-        ls *= b;
-        ot.x *= b; ot.y *= b; ot.z *= b; ot.w *= b;
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const float f = ex2(ml[u].x - ref);
-            ls = fmaf(ml[u].y, f, ls);
-            ot.x = fmaf(v[u].x, f, ot.x); ot.y = fmaf(v[u].y, f, ot.y); ot.z = fmaf(v[u].z, f, ot.z); ot.w = fmaf(v[u].w, f, ot.w);
-        }
-    }
-    so[stripe][lane] = ot;
-    if (lane == 0) sml[stripe] = make_float2(mt, ls);
-    __syncthreads();
-    if (stripe == 0) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < kStripes; ++k) mx = fmaxf(mx, sml[k].x);
-        const float ref = mx == -INFINITY ? 0.f : mx;
-        ls = 0.f;
-        ot = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < kStripes; ++k) {
-            const float f = ex2(sml[k].x - ref);
-            const float4 v = so[k][lane];
-            ls = fmaf(sml[k].y, f, ls);
-            ot.x = fmaf(v.x, f, ot.x); ot.y = fmaf(v.y, f, ot.y); ot.z = fmaf(v.z, f, ot.z); ot.w = fmaf(v.w, f, ot.w);
-        }
-        const float inv = ls == 0.f ? 0.f : 1.f / ls;
-        *reinterpret_cast<uint2 *>(out + ((size_t)head * G + g) * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
-        if (lse && c == 0) lse[(size_t)head * G + g] = ls == 0.f ? -INFINITY : (mx + log2f(ls)) * kLn2;
-    }
-}
-
 int shares_for(const PagedProblem &p, int per_sm, int unit)
 {
     // (a unit for a share at least, at the lengths that the table has room for)
@@ -929,8 +926,8 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     constexpr auto clusters = [] { if constexpr (kInt4) return paged_decode4_kernel<D, NQ, true>; else return paged_decode16_kernel<D, NQ, true>; }();
     const int G = p.H / p.pool.Hkv, sms = device_info().sms, shares = shares_for(p, C::kShares, C::kUnitKeys), most = 4 * sms;
     const int heads = p.B * p.pool.Hkv, slots = C::kCtas * sms, units = (int)(((long long)p.max_pages * p.pool.page + C::kUnitKeys - 1) / C::kUnitKeys);
-    // A cluster for each head, and no merge kernel, while all of them fit at once (clusters of 4 and 8 leave SMs of a GPC over) and a CTA does not stream
-    // more than 192 KB beyond an equal share of what the tables have room for, about what the merge kernel costs.
+    // A cluster for each head, and no counters, while all of them fit at once (clusters of 4 and 8 leave SMs of a GPC over) and a CTA does not stream
+    // more than 192 KB beyond an equal share of what the tables have room for, about what the clearing and the joins cost.
     int cl = 0;
     for (int c = 1; c <= 8 && (long long)heads * c * 100 <= slots * (c == 8 ? 85LL : c == 4 ? 90LL : 100LL); c *= 2) cl = c;
     const long long mine = cl ? (units + cl - 1) / cl : 0, equal = ((long long)units * heads + slots - 1) / slots;
@@ -941,7 +938,7 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     a.out = (__nv_bfloat16 *)out; a.lse = lse;
     a.part_o = (float *)ws;
     a.part_ml = a.part_o + (size_t)2 * most * G * D;
-    a.info = (int2 *)(a.part_ml + (size_t)2 * most * G * 2);
+    a.counters = (unsigned int *)(a.part_ml + (size_t)2 * most * G * 2);
     a.sq = p.sq;
     a.table_stride = p.table_stride; a.page_stride = p.pool.page_stride;
     a.B = p.B; a.Hkv = p.pool.Hkv; a.G = G; a.pages = p.pool.pages; a.page = p.pool.page;
@@ -951,18 +948,13 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     a.cl = cl;
     a.scale_log2 = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
     a.sign2 = p.scale == 0.f ? 0u : p.scale > 0.f ? 0x3f803f80u : 0xbf80bf80u;
-    const cudaError_t e = cl ? allow_smem<clusters>(C::kTotal) : allow_smem<kernel>(C::kTotal);
+    cudaError_t e = cl ? allow_smem<clusters>(C::kTotal) : allow_smem<kernel>(C::kTotal);
+    if (e == cudaSuccess && !cl) e = decode_clear(a.counters, most, st);
     if (e != cudaSuccess) return e;
-    {
-        LaunchScope scope(MOA_KERNEL_OTHER, st);
-        const dim3 grid((unsigned)ctas), block(C::kThreads);
-        const cudaError_t le = cl ? launch_cluster(clusters, (unsigned)cl, grid, block, (size_t)C::kTotal, st, a)
-                                  : launch_dependent(kernel, grid, block, (size_t)C::kTotal, st, a);
-        if (le != cudaSuccess || cl) return le;
-    }
     LaunchScope scope(MOA_KERNEL_OTHER, st);
-    return launch_dependent(paged_merge_kernel<D>, dim3((unsigned)std::min(shares, ctas * C::kTeams), (unsigned)G), dim3(128), (size_t)0, st, (const int2 *)a.info, (const float *)a.part_o,
-                            (const float *)a.part_ml, (__nv_bfloat16 *)out, lse, G);
+    const dim3 grid((unsigned)ctas), block(C::kThreads);
+    return cl ? launch_cluster(clusters, (unsigned)cl, grid, block, (size_t)C::kTotal, st, a)
+              : launch_dependent(kernel, grid, block, (size_t)C::kTotal, st, a);
 }
 
 }  // namespace
@@ -970,7 +962,7 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
 size_t paged_decode_workspace_bytes(const PagedProblem &p)
 {
     const size_t most = (size_t)4 * device_info().sms, G = (size_t)(p.H / p.pool.Hkv);
-    return 2 * most * G * (p.pool.d + 2) * sizeof(float) + most * sizeof(int2);
+    return 2 * most * G * (p.pool.d + 2) * sizeof(float) + most * sizeof(unsigned int);
 }
 
 cudaError_t paged_decode(const PagedProblem &p, const void *q, const void *pool, const int *table, const int *lens, void *out, float *lse,
