@@ -4,8 +4,9 @@
 // a 64-bit product and a sine and cosine of about 60 instructions, against H + H_k heads that share them.  So a block of two warps takes a token
 // with all its heads, makes each angle once (one per thread at d_rot = 128) and keeps them in shared memory; a row of a head is then d / 16 lanes with
 // the two 16-byte pieces of it that rotate into each other, two rows in flight per lane.  Small blocks, twenty to an SM: while one makes its angles others
-// stream, and the last round of blocks is short (B2 n4096 H16/16 d128, 134 MB: 23.4 us, 5.7 TB/s; four tokens to 256 threads 23.8; 3001 tokens of
-// fp32 H8/2 d80 4.3 and 4.9; equal shares of the tokens for the resident blocks 25; four rows in flight 24.0).
+// stream, and the last round of blocks is short; the first rows are on their way while the angles are made (B2 n4096 H16/16 d128, 134 MB: 22.6 us, 5.9 TB/s;
+// with the loads behind the angles 23.5, with 16 or 18 blocks to an SM 23.2 and 23.9, four tokens to 256 threads 23.8; 3001 tokens of
+// fp32 H8/2 d80 4.1, behind the angles 4.6; equal shares of the tokens for the resident blocks 25; four rows in flight 24.0).
 // No table of angles: one would be read per token and head size, needs a largest position, and is not faster than what hides under the
 // loads here.
 #include "rotate.cuh"
@@ -39,6 +40,27 @@ __global__ void __launch_bounds__(kThreads, kResident) rope_kernel(const RopeArg
     grid_launch_dependents();
     const int at = after_wait(a.pos)[t];
     const float *inv_freq = after_wait(a.inv_freq);
+    const int r0 = (int)a.by_lanes.div((uint32_t)tid), p = tid - r0 * a.lanes, per = kThreads / a.lanes;
+    const bool turns = p < a.np;
+    const int c0 = turns && !kPairs ? p * V : 2 * p * V, c1 = turns && !kPairs ? freqs + p * V : c0 + V;
+    const bool two = c1 < a.d;       // (what is not turned may end with a single piece)
+    const int rows = r0 < per ? a.rows : 0;
+    const T *q = after_wait((const T *)a.q) + (long long)t * a.sq.token, *k = after_wait((const T *)a.k) + (long long)t * a.sk.token;
+    T *qo = (T *)a.qo + (long long)t * a.so.token, *ko = (T *)a.ko + (long long)t * a.sko.token;
+    Chunk<T, V> x[kUnroll], y[kUnroll];
+    auto load = [&](int r) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int h = r + u * per, hk = h - a.H;
+            if (h < rows) {
+                const T *src = hk < 0 ? q + (long long)h * a.sq.head : k + (long long)hk * a.sk.head;
+                x[u] = *reinterpret_cast<const Chunk<T, V> *>(src + c0);
+                if (two) y[u] = *reinterpret_cast<const Chunk<T, V> *>(src + c1);
+            }
+        }
+    };
+    int r = r0 + (int)blockIdx.y * per * kUnroll;
+    load(r);
     for (int f = tid; f < freqs; f += kThreads) {
         float2 cs = position_angle(at, inv_freq[f]);
         cs.x *= a.factor;
@@ -46,30 +68,12 @@ __global__ void __launch_bounds__(kThreads, kResident) rope_kernel(const RopeArg
         write_angle<V>(angles, a.np, f, cs);
     }
     __syncthreads();
-    const int r0 = (int)a.by_lanes.div((uint32_t)tid), p = tid - r0 * a.lanes, per = kThreads / a.lanes;
-    if (r0 >= per) return;
-    const bool turns = p < a.np;
-    const int c0 = turns && !kPairs ? p * V : 2 * p * V, c1 = turns && !kPairs ? freqs + p * V : c0 + V;
-    const bool two = c1 < a.d;       // (what is not turned may end with a single piece)
-    const T *q = after_wait((const T *)a.q) + (long long)t * a.sq.token, *k = after_wait((const T *)a.k) + (long long)t * a.sk.token;
-    T *qo = (T *)a.qo + (long long)t * a.so.token, *ko = (T *)a.ko + (long long)t * a.sko.token;
-    for (int r = r0 + (int)blockIdx.y * per * kUnroll; r < a.rows; r += per * kUnroll * (int)gridDim.y) {
-        Chunk<T, V> x[kUnroll], y[kUnroll];
-        T *dst[kUnroll];
+    while (r < rows) {
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const int h = r + u * per, hk = h - a.H;
-            dst[u] = nullptr;
-            if (h < a.rows) {
-                const T *src = hk < 0 ? q + (long long)h * a.sq.head : k + (long long)hk * a.sk.head;
-                dst[u] = hk < 0 ? qo + (long long)h * a.so.head : ko + (long long)hk * a.sko.head;
-                x[u] = *reinterpret_cast<const Chunk<T, V> *>(src + c0);
-                if (two) y[u] = *reinterpret_cast<const Chunk<T, V> *>(src + c1);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            if (!dst[u]) continue;
+            if (h >= rows) continue;
+            T *dst = hk < 0 ? qo + (long long)h * a.so.head : ko + (long long)hk * a.sko.head;
             if (turns) {
                 float fx[V], fy[V], c[V], s[V];
                 read_angles<V>(angles, a.np, p, c, s);
@@ -79,9 +83,11 @@ __global__ void __launch_bounds__(kThreads, kResident) rope_kernel(const RopeArg
                 x[u].pack(fx);
                 y[u].pack(fy);
             }
-            *reinterpret_cast<Chunk<T, V> *>(dst[u] + c0) = x[u];
-            if (two) *reinterpret_cast<Chunk<T, V> *>(dst[u] + c1) = y[u];
+            *reinterpret_cast<Chunk<T, V> *>(dst + c0) = x[u];
+            if (two) *reinterpret_cast<Chunk<T, V> *>(dst + c1) = y[u];
         }
+        r += per * kUnroll * (int)gridDim.y;
+        load(r);
     }
 }
 
