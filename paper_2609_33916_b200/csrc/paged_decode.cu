@@ -22,6 +22,7 @@
 #include "cache_layout.cuh"
 #include "ptx.cuh"
 #include <algorithm>
+#include <cmath>
 
 namespace moa {
 namespace {
@@ -44,7 +45,7 @@ struct PagedArgs {
     long long table_stride, page_stride;
     int B, Hkv, G, pages, page, cap;      // cap: keys that a row of the table has room for
     FastDiv by_page;
-    int cl;                     // CTAs of a head's cluster; 0: no clusters
+    int cl, nc;                 // CTAs of a cluster, clusters of a head; 0: no clusters
     float scale_log2;           // > 0; the sign (or 0) is q's factor, a pair of bf16
     uint32_t sign2;
     unsigned int *status;
@@ -201,11 +202,12 @@ template <class C> __device__ __forceinline__ Share find_share(const PagedArgs &
     return s;
 }
 
-// With clusters: CTA rank r of a head's cluster, team k: part r * kTeams + k of the head's units
+// With clusters: CTA rank r of a head's j-th cluster, team k: part (j * cl + r) * kTeams + k of the head's units
 template <class C> __device__ __forceinline__ Share cluster_share(const PagedArgs &a, const int *lens, int team)
 {
     Share s;
-    const int head = (int)blockIdx.x / a.cl, parts = a.cl * C::kTeams, part = (int)cluster_ctarank() * C::kTeams + team;
+    const int cluster = (int)blockIdx.x / a.cl, head = cluster / a.nc, parts = a.nc * a.cl * C::kTeams;
+    const int part = ((cluster - head * a.nc) * a.cl + (int)cluster_ctarank()) * C::kTeams + team;
     s.b = head / a.Hkv;
     const int n = units_of<C::kUnitKeys>(min(lens[s.b], a.cap));
     s.units = n * a.Hkv;
@@ -559,11 +561,70 @@ __device__ __forceinline__ int share_of(const Share &sh, int u)
     return c;
 }
 
+// Four elements of a query, from c on, of `parts` partial results: slot(k) says where part k is.  Thread `lane` of the `lanes` (a power of two, neighbours
+// in a warp) that share them; all of them get the result.
+struct Joined {
+    float m, l;
+    float4 o;
+};
+template <int D, class Slot>
+__device__ __forceinline__ Joined join_parts(const PagedArgs &a, int g, int c, int parts, int lane, int lanes, Slot slot)
+{
+    constexpr int kBatch = 8;
+    Joined r{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    auto add = [&](float m, float l, const float4 &v, float ref) {
+        const float f = ex2(m - ref);
+        r.l = fmaf(l, f, r.l);
+        r.o.x = fmaf(v.x, f, r.o.x); r.o.y = fmaf(v.y, f, r.o.y); r.o.z = fmaf(v.z, f, r.o.z); r.o.w = fmaf(v.w, f, r.o.w);
+    };
+    auto rescale = [&](float mn) {
+        const float ref = mn == -INFINITY ? 0.f : mn, b = ex2(r.m - ref);
+        r.m = mn;
+        r.l *= b;
+        r.o.x *= b; r.o.y *= b; r.o.z *= b; r.o.w *= b;
+        return ref;
+    };
+    for (int k0 = lane; k0 < parts; k0 += lanes * kBatch) {
+        float2 ml[kBatch];
+        float4 v[kBatch];
+        float mn = r.m;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const bool there = k0 + u * lanes < parts;
+            const size_t at = (size_t)slot(k0 + u * lanes) * a.G + g;
+            ml[u] = there ? __ldcg(reinterpret_cast<const float2 *>(a.part_ml + at * 2)) : make_float2(-INFINITY, 0.f);
+            v[u] = there ? __ldcg(reinterpret_cast<const float4 *>(a.part_o + at * D + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, ml[u].x);
+        const float ref = rescale(mn);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) add(ml[u].x, ml[u].y, v[u], ref);
+    }
+    for (int o = 1; o < lanes; o <<= 1) {
+        const float m = __shfl_xor_sync(0xffffffffu, r.m, o), ref = rescale(fmaxf(r.m, m));
+        // (both sides on the same reference: their sums add)
+        (void)ref;
+        r.l += __shfl_xor_sync(0xffffffffu, r.l, o);
+        r.o.x += __shfl_xor_sync(0xffffffffu, r.o.x, o); r.o.y += __shfl_xor_sync(0xffffffffu, r.o.y, o);
+        r.o.z += __shfl_xor_sync(0xffffffffu, r.o.z, o); r.o.w += __shfl_xor_sync(0xffffffffu, r.o.w, o);
+    }
+    return r;
+}
+template <int D>
+__device__ __forceinline__ void write_result(const PagedArgs &a, int head, int g, int c, const Joined &r)
+{
+    const size_t at = (size_t)head * a.G + g;
+    const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
+    *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(r.o.x * inv, r.o.y * inv), pack_bf16(r.o.z * inv, r.o.w * inv));
+    if (a.lse && c == 0) a.lse[at] = r.l == 0.f ? -INFINITY : (r.m + log2f(r.l)) * kLn2;
+}
+
 // A head that lies in several shares, ca to cb: the team that leaves its part last joins them all (nobody waits for anyone).
 template <int D, class C>
 __device__ __forceinline__ void last_joins(const PagedArgs &a, int team, int head, int ca, int cb, unsigned int *flag)
 {
-    constexpr int kJoin = 32 * kWarps, kBatch = 4;
+    constexpr int kJoin = 32 * kWarps;
     const int tid = threadIdx.x % kJoin;
     __threadfence();                            // (this thread's part, before the count)
     named_barrier(1 + team, kJoin);
@@ -571,38 +632,11 @@ __device__ __forceinline__ void last_joins(const PagedArgs &a, int team, int hea
     named_barrier(1 + team, kJoin);
     if (*flag != (unsigned)(cb - ca)) return;
     __threadfence();
-    for (int idx = tid; idx < a.G * (D / 4); idx += kJoin) {
+    const int all = a.G * (D / 4);
+    for (int idx = tid; idx < all; idx += kJoin) {
         const int g = idx / (D / 4), c = 4 * (idx % (D / 4));
-        float mt = -INFINITY, ls = 0.f;
-        float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k0 = ca; k0 <= cb; k0 += kBatch) {
-            float2 ml[kBatch];
-            float4 v[kBatch];
-            float mn = mt;
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const size_t at = (size_t)(2 * (k0 + u) + (k0 + u == ca ? 1 : 0)) * a.G + g;
-                const bool there = k0 + u <= cb;
-                ml[u] = there ? __ldcg(reinterpret_cast<const float2 *>(a.part_ml + at * 2)) : make_float2(-INFINITY, 0.f);
-                v[u] = there ? __ldcg(reinterpret_cast<const float4 *>(a.part_o + at * D + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, ml[u].x);
-            const float ref = mn == -INFINITY ? 0.f : mn, b = ex2(mt - ref);
-            mt = mn;
-            ls *= b;
-            ot.x *= b; ot.y *= b; ot.z *= b; ot.w *= b;
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const float f = ex2(ml[u].x - ref);
-                ls = fmaf(ml[u].y, f, ls);
-                ot.x = fmaf(v[u].x, f, ot.x); ot.y = fmaf(v[u].y, f, ot.y); ot.z = fmaf(v[u].z, f, ot.z); ot.w = fmaf(v[u].w, f, ot.w);
-            }
-        }
-        const size_t at = (size_t)head * a.G + g;
-        const float inv = ls == 0.f ? 0.f : 1.f / ls;
-        *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
-        if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + log2f(ls)) * kLn2;
+        const Joined r = join_parts<D>(a, g, c, cb - ca + 1, 0, 1, [&](int k) { return 2 * (ca + k) + (k == 0 ? 1 : 0); });
+        write_result<D>(a, head, g, c, r);
     }
 }
 
@@ -648,7 +682,7 @@ template <int D, bool kInt4, int NQ>
 __device__ __forceinline__ void combine(const PagedArgs &a, uint8_t *shared, int tid, int threads)
 {
     using C = Cfg<D, kInt4, NQ>;
-    const int head = (int)blockIdx.x / a.cl, rank = (int)cluster_ctarank(), all = a.G * (D / 4), k = tid % 8;
+    const int cluster = (int)blockIdx.x / a.cl, rank = (int)cluster_ctarank(), all = a.G * (D / 4), k = tid % 8;
     const int first = all * rank / a.cl, last = all * (rank + 1) / a.cl;
     const uint32_t base = smem_u32(shared);
     for (int i0 = first; i0 < last; i0 += threads / 8) {       // (whole warps: the exchanges below)
@@ -687,11 +721,43 @@ __device__ __forceinline__ void combine(const PagedArgs &a, uint8_t *shared, int
             ot.z += __shfl_xor_sync(0xffffffffu, ot.z, o); ot.w += __shfl_xor_sync(0xffffffffu, ot.w, o);
         }
         if (in && k == 0) {
-            const size_t at = (size_t)head * a.G + r;
-            const float inv = ls == 0.f ? 0.f : 1.f / ls;
-            *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
-            if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + log2f(ls)) * kLn2;
+            if (a.nc == 1) {
+                write_result<D>(a, cluster, r, c, Joined{mt, ls, ot});
+            } else {
+                const size_t at = (size_t)cluster * a.G + r;
+                *reinterpret_cast<float4 *>(a.part_o + at * D + c) = ot;
+                if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(mt, ls);
+            }
         }
+    }
+}
+
+// The end of a cluster kernel, for every thread of the cluster: the teams' rows joined, and where a head has several clusters, their partial results by the
+// last of them to come, all its CTAs.  `flag` lies behind what combine() reads.  Threads that only load (tid < 0) keep the barriers company.
+template <int D, bool kInt4, int NQ>
+__device__ __forceinline__ void finish_clusters(const PagedArgs &a, uint8_t *shared, unsigned int *flag, int tid, int threads)
+{
+    cluster_sync_all();
+    if (tid >= 0) combine<D, kInt4, NQ>(a, shared, tid, threads);
+    if (a.nc > 1) __threadfence();                             // (this thread's part, before the count)
+    __syncwarp();
+    cluster_sync_all();                                        // nobody leaves while another CTA may still read its shared memory
+    if (a.nc == 1) return;
+    const int head = (int)blockIdx.x / (a.cl * a.nc), rank = (int)cluster_ctarank();
+    if (tid == 0 && rank == 0) *flag = atomicAdd(a.counters + head, 1u);
+    __syncwarp();
+    cluster_sync_all();
+    unsigned int came;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(came) : "r"(mapa_u32(smem_u32(flag), 0u)) : "memory");
+    __syncwarp();
+    cluster_sync_all();
+    if (tid < 0 || came != (unsigned)(a.nc - 1)) return;
+    __threadfence();
+    const int all = a.G * (D / 4), first = all * rank / a.cl, last = all * (rank + 1) / a.cl;
+    for (int i0 = first; i0 < last; i0 += threads / 4) {       // (whole warps: the exchanges)
+        const int idx = i0 + tid / 4, at = min(idx, last - 1), g = at / (D / 4), c = 4 * (at % (D / 4));
+        const Joined r = join_parts<D>(a, g, c, a.nc, tid % 4, 4, [&](int k) { return head * a.nc + k; });
+        if (idx < last && tid % 4 == 0) write_result<D>(a, head, g, c, r);
     }
 }
 
@@ -714,8 +780,8 @@ __global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ
         *abortp = 0;
         fence_mbar_init();
     }
-    // (without clusters the kernel in front is the one that clears the counters: only who uses them waits for it)
-    if constexpr (kClusters) {
+    // (unless a cluster does a whole head, the kernel in front is the one that clears the counters: only who uses them waits for it)
+    if (kClusters && a.nc == 1) {
         grid_dependency_wait();
         grid_launch_dependents();
     }
@@ -775,17 +841,14 @@ __global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ
             if (lane == 0) mbar_drain(full, armed);      // copies still on their way land before the CTA leaves (bounded)
         }
         __syncwarp();
-        if constexpr (kClusters) {
-            cluster_sync_all();
-            cluster_sync_all();
-        }
+        if constexpr (kClusters) finish_clusters<D, true, NQ>(a, shared, reinterpret_cast<unsigned int *>(shared + C::offFlag), -1, 128 * C::kTeams);
         return;
     }
 
     // ---------------------------------------------------------------------- use
     const float scale = a.scale_log2 * exp2i(-kCodeExp1 - kLift), margin = kRescale / scale;
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kUseRegs));
-    if constexpr (!kClusters) {
+    if (!kClusters || a.nc > 1) {
         grid_dependency_wait();
         grid_launch_dependents();
     }
@@ -804,10 +867,7 @@ __global__ void __launch_bounds__((Cfg<D, true, NQ>::kThreads), (Cfg<D, true, NQ
     });
     if constexpr (kClusters) {
         __syncwarp();
-        cluster_sync_all();
-        combine<D, true, NQ>(a, shared, tid, 128 * C::kTeams);
-        __syncwarp();
-        cluster_sync_all();      // nobody leaves while another CTA may still read its shared memory
+        finish_clusters<D, true, NQ>(a, shared, reinterpret_cast<unsigned int *>(shared + C::offFlag), tid, 128 * C::kTeams);
     }
 }
 
@@ -818,8 +878,8 @@ __global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, 
     constexpr int S = C::kStages;
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid % 32;
-    // (without clusters the kernel in front is the one that clears the counters)
-    if constexpr (kClusters) {
+    // (unless a cluster does a whole head, the kernel in front is the one that clears the counters: only who uses them waits for it)
+    if (kClusters && a.nc == 1) {
         grid_dependency_wait();
         grid_launch_dependents();
     }
@@ -885,7 +945,7 @@ __global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, 
     for (int i = 0; i < S - 1; ++i) request(i);
 
     // ---- use
-    if constexpr (!kClusters) {
+    if (!kClusters || a.nc > 1) {
         grid_dependency_wait();
         grid_launch_dependents();
     }
@@ -901,10 +961,7 @@ __global__ void __launch_bounds__((Cfg<D, false, NQ>::kThreads), (Cfg<D, false, 
     });
     if constexpr (kClusters) {
         __syncwarp();
-        cluster_sync_all();
-        combine<D, false, NQ>(a, smem, tid, 128);
-        __syncwarp();
-        cluster_sync_all();      // nobody leaves while another CTA may still read its shared memory
+        finish_clusters<D, false, NQ>(a, smem, reinterpret_cast<unsigned int *>(smem + C::offFlag), tid, 128);
     } else {
         cp_wait<0>();
     }
@@ -925,14 +982,31 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     constexpr auto kernel = [] { if constexpr (kInt4) return paged_decode4_kernel<D, NQ, false>; else return paged_decode16_kernel<D, NQ, false>; }();
     constexpr auto clusters = [] { if constexpr (kInt4) return paged_decode4_kernel<D, NQ, true>; else return paged_decode16_kernel<D, NQ, true>; }();
     const int G = p.H / p.pool.Hkv, sms = device_info().sms, shares = shares_for(p, C::kShares, C::kUnitKeys), most = 4 * sms;
+    // One or more clusters for each head, or equal shares of everything.  Clusters that run at once: those of 4 and 8 leave SMs of a GPC over.  In
+    // nanoseconds, for the lengths that the tables have room for: an SM streams about 40 bytes in one; one cluster for a head needs no counters and no second
+    // join; shares of few heads are many parts, which one team joins 32 at a time and 32 elements at once.
+    // Equal shares of everything, or one or more clusters for each head: by the time that each takes in nanoseconds, for the lengths that the tables have room
+    // for.  HBM gives 6500 bytes in one; an SM takes 60, of 4-bit blocks 38 (it computes for longer).  One cluster for a head needs no counters
+    // and no second join; shares of few heads are many parts, which one team joins, 128 elements at once and eight parts on their way.  Clusters of 4 and 8
+    // leave SMs of a GPC over.  (B8 H8/8 n8192 d128 bf16: clusters of four 43 us, shares 48; B1 H8/1 n131072 4 bits: 15 clusters of eight 15 us, one
+    // cluster 60, shares 92; B64 H32/8 of 4000 keys 4 bits: shares 78, clusters do not fit.)
     const int heads = p.B * p.pool.Hkv, slots = C::kCtas * sms, units = (int)(((long long)p.max_pages * p.pool.page + C::kUnitKeys - 1) / C::kUnitKeys);
-    // A cluster for each head, and no counters, while all of them fit at once (clusters of 4 and 8 leave SMs of a GPC over) and a CTA does not stream
-    // more than 192 KB beyond an equal share of what the tables have room for, about what the clearing and the joins cost.
-    int cl = 0;
-    for (int c = 1; c <= 8 && (long long)heads * c * 100 <= slots * (c == 8 ? 85LL : c == 4 ? 90LL : 100LL); c *= 2) cl = c;
-    const long long mine = cl ? (units + cl - 1) / cl : 0, equal = ((long long)units * heads + slots - 1) / slots;
-    if (cl && (mine - equal) * C::kBlocks * C::kBlock > 192 * 1024) cl = 0;
-    const int ctas = cl ? heads * cl : std::min(shares, slots);
+    constexpr double kUnitBytes = (double)C::kBlocks * C::kBlock, kSmRate = kInt4 ? 38.0 : 60.0;
+    const double hbm = kUnitBytes * units * heads / 6500.0;
+    auto stream = [&](double units_of_a_team, double teams_on_an_sm) { return std::max(hbm, std::ceil(units_of_a_team) * kUnitBytes * teams_on_an_sm / kSmRate); };
+    const double equal = std::max(1.0, (double)units * heads / (C::kShares * sms)), parts = std::min((double)units, std::max(1.0, (double)C::kShares * sms / heads));
+    double best = stream(equal, C::kShares) + 2500.0 + 700.0 * std::ceil(parts / 8.0) * ((G * (D / 4) + 127) / 128);
+    int cl = 0, nc = 0;
+    for (int c = 1; c <= 8; c *= 2) {
+        const long long at_once = slots * (c == 8 ? 85LL : c == 4 ? 90LL : 100LL) / (100LL * c);
+        if (heads > at_once) break;
+        const int most = (int)std::min<long long>(at_once / heads, (units + c * C::kTeams - 1) / (c * C::kTeams));
+        for (int n : {1, most}) {
+            const double cost = stream((double)units / (n * c * C::kTeams), (double)((heads * n * c + sms - 1) / sms) * C::kTeams) + (n > 1 ? 5000.0 : 1500.0);
+            if (cost < best || (cost == best && cl)) { best = cost; cl = c; nc = n; }
+        }
+    }
+    const int ctas = cl ? heads * nc * cl : std::min(shares, slots);
     PagedArgs a{};
     a.q = (const __nv_bfloat16 *)q; a.pool = (const uint8_t *)pool; a.table = table; a.lens = lens;
     a.out = (__nv_bfloat16 *)out; a.lse = lse;
@@ -946,10 +1020,11 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     a.by_page = FastDiv((uint32_t)p.pool.page);
     a.status = device_status_ptr();
     a.cl = cl;
+    a.nc = nc;
     a.scale_log2 = p.scale == 0.f ? 1.f : fabsf(p.scale) * kLog2e;
     a.sign2 = p.scale == 0.f ? 0u : p.scale > 0.f ? 0x3f803f80u : 0xbf80bf80u;
     cudaError_t e = cl ? allow_smem<clusters>(C::kTotal) : allow_smem<kernel>(C::kTotal);
-    if (e == cudaSuccess && !cl) e = decode_clear(a.counters, most, st);
+    if (e == cudaSuccess && (!cl || nc > 1)) e = decode_clear(a.counters, most, st);
     if (e != cudaSuccess) return e;
     LaunchScope scope(MOA_KERNEL_OTHER, st);
     const dim3 grid((unsigned)ctas), block(C::kThreads);
