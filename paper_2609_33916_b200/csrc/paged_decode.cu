@@ -561,55 +561,53 @@ __device__ __forceinline__ int share_of(const Share &sh, int u)
     return c;
 }
 
-// Four elements of a query, from c on, of `parts` partial results: slot(k) says where part k is.  Thread `lane` of the `lanes` (a power of two, neighbours
-// in a warp) that share them; all of them get the result.
+// Four elements of a query, from c on, of `parts` partial results: slot(k) says where part k is; kBatch of them on their way.  Thread `lane` of the kLanes
+// (neighbours in a warp) that share them; all of them get the result.
 struct Joined {
     float m, l;
     float4 o;
 };
-template <int D, class Slot>
-__device__ __forceinline__ Joined join_parts(const PagedArgs &a, int g, int c, int parts, int lane, int lanes, Slot slot)
+template <int D, int kLanes, int kBatch, class Slot>
+__device__ __forceinline__ Joined join_parts(const PagedArgs &a, int g, int c, int parts, int lane, Slot slot)
 {
-    constexpr int kBatch = 8;
-    Joined r{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-    auto add = [&](float m, float l, const float4 &v, float ref) {
-        const float f = ex2(m - ref);
-        r.l = fmaf(l, f, r.l);
-        r.o.x = fmaf(v.x, f, r.o.x); r.o.y = fmaf(v.y, f, r.o.y); r.o.z = fmaf(v.z, f, r.o.z); r.o.w = fmaf(v.w, f, r.o.w);
-    };
-    auto rescale = [&](float mn) {
-        const float ref = mn == -INFINITY ? 0.f : mn, b = ex2(r.m - ref);
-        r.m = mn;
-        r.l *= b;
-        r.o.x *= b; r.o.y *= b; r.o.z *= b; r.o.w *= b;
-        return ref;
-    };
-    for (int k0 = lane; k0 < parts; k0 += lanes * kBatch) {
+    float mt = -INFINITY, ls = 0.f;
+    float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = lane; k0 < parts; k0 += kLanes * kBatch) {
         float2 ml[kBatch];
         float4 v[kBatch];
-        float mn = r.m;
+        float mn = mt;
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const bool there = k0 + u * lanes < parts;
-            const size_t at = (size_t)slot(k0 + u * lanes) * a.G + g;
+            const bool there = k0 + u * kLanes < parts;
+            const size_t at = (size_t)slot(k0 + u * kLanes) * a.G + g;
             ml[u] = there ? __ldcg(reinterpret_cast<const float2 *>(a.part_ml + at * 2)) : make_float2(-INFINITY, 0.f);
             v[u] = there ? __ldcg(reinterpret_cast<const float4 *>(a.part_o + at * D + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, ml[u].x);
-        const float ref = rescale(mn);
+        const float ref = mn == -INFINITY ? 0.f : mn, b = ex2(mt - ref);
+        mt = mn;
+        ls *= b;
+        ot.x *= b; ot.y *= b; ot.z *= b; ot.w *= b;
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) add(ml[u].x, ml[u].y, v[u], ref);
+        for (int u = 0; u < kBatch; ++u) {
+            const float f = ex2(ml[u].x - ref);
+            ls = fmaf(ml[u].y, f, ls);
+            ot.x = fmaf(v[u].x, f, ot.x); ot.y = fmaf(v[u].y, f, ot.y); ot.z = fmaf(v[u].z, f, ot.z); ot.w = fmaf(v[u].w, f, ot.w);
+        }
     }
-    for (int o = 1; o < lanes; o <<= 1) {
-        const float m = __shfl_xor_sync(0xffffffffu, r.m, o), ref = rescale(fmaxf(r.m, m));
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1) {
         // (both sides on the same reference: their sums add)
-        (void)ref;
-        r.l += __shfl_xor_sync(0xffffffffu, r.l, o);
-        r.o.x += __shfl_xor_sync(0xffffffffu, r.o.x, o); r.o.y += __shfl_xor_sync(0xffffffffu, r.o.y, o);
-        r.o.z += __shfl_xor_sync(0xffffffffu, r.o.z, o); r.o.w += __shfl_xor_sync(0xffffffffu, r.o.w, o);
+        const float mn = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, o)), b = ex2(mt - (mn == -INFINITY ? 0.f : mn));
+        mt = mn;
+        ls *= b;
+        ot.x *= b; ot.y *= b; ot.z *= b; ot.w *= b;
+        ls += __shfl_xor_sync(0xffffffffu, ls, o);
+        ot.x += __shfl_xor_sync(0xffffffffu, ot.x, o); ot.y += __shfl_xor_sync(0xffffffffu, ot.y, o);
+        ot.z += __shfl_xor_sync(0xffffffffu, ot.z, o); ot.w += __shfl_xor_sync(0xffffffffu, ot.w, o);
     }
-    return r;
+    return Joined{mt, ls, ot};
 }
 template <int D>
 __device__ __forceinline__ void write_result(const PagedArgs &a, int head, int g, int c, const Joined &r)
@@ -624,7 +622,7 @@ __device__ __forceinline__ void write_result(const PagedArgs &a, int head, int g
 template <int D, class C>
 __device__ __forceinline__ void last_joins(const PagedArgs &a, int team, int head, int ca, int cb, unsigned int *flag)
 {
-    constexpr int kJoin = 32 * kWarps;
+    constexpr int kJoin = 32 * kWarps, kBatch = 4;
     const int tid = threadIdx.x % kJoin;
     __threadfence();                            // (this thread's part, before the count)
     named_barrier(1 + team, kJoin);
@@ -632,11 +630,38 @@ __device__ __forceinline__ void last_joins(const PagedArgs &a, int team, int hea
     named_barrier(1 + team, kJoin);
     if (*flag != (unsigned)(cb - ca)) return;
     __threadfence();
-    const int all = a.G * (D / 4);
-    for (int idx = tid; idx < all; idx += kJoin) {
+    for (int idx = tid; idx < a.G * (D / 4); idx += kJoin) {
         const int g = idx / (D / 4), c = 4 * (idx % (D / 4));
-        const Joined r = join_parts<D>(a, g, c, cb - ca + 1, 0, 1, [&](int k) { return 2 * (ca + k) + (k == 0 ? 1 : 0); });
-        write_result<D>(a, head, g, c, r);
+        float mt = -INFINITY, ls = 0.f;
+        float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k0 = ca; k0 <= cb; k0 += kBatch) {
+            float2 ml[kBatch];
+            float4 v[kBatch];
+            float mn = mt;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const size_t at = (size_t)(2 * (k0 + u) + (k0 + u == ca ? 1 : 0)) * a.G + g;
+                const bool there = k0 + u <= cb;
+                ml[u] = there ? __ldcg(reinterpret_cast<const float2 *>(a.part_ml + at * 2)) : make_float2(-INFINITY, 0.f);
+                v[u] = there ? __ldcg(reinterpret_cast<const float4 *>(a.part_o + at * D + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, ml[u].x);
+            const float ref = mn == -INFINITY ? 0.f : mn, b = ex2(mt - ref);
+            mt = mn;
+            ls *= b;
+            ot.x *= b; ot.y *= b; ot.z *= b; ot.w *= b;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const float f = ex2(ml[u].x - ref);
+                ls = fmaf(ml[u].y, f, ls);
+                ot.x = fmaf(v[u].x, f, ot.x); ot.y = fmaf(v[u].y, f, ot.y); ot.z = fmaf(v[u].z, f, ot.z); ot.w = fmaf(v[u].w, f, ot.w);
+            }
+        }
+        const size_t at = (size_t)head * a.G + g;
+        const float inv = ls == 0.f ? 0.f : 1.f / ls;
+        *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
+        if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + log2f(ls)) * kLn2;
     }
 }
 
@@ -756,7 +781,7 @@ __device__ __forceinline__ void finish_clusters(const PagedArgs &a, uint8_t *sha
     const int all = a.G * (D / 4), first = all * rank / a.cl, last = all * (rank + 1) / a.cl;
     for (int i0 = first; i0 < last; i0 += threads / 4) {       // (whole warps: the exchanges)
         const int idx = i0 + tid / 4, at = min(idx, last - 1), g = at / (D / 4), c = 4 * (at % (D / 4));
-        const Joined r = join_parts<D>(a, g, c, a.nc, tid % 4, 4, [&](int k) { return head * a.nc + k; });
+        const Joined r = join_parts<D, 4, 4>(a, g, c, a.nc, tid % 4, [&](int k) { return head * a.nc + k; });
         if (idx < last && tid % 4 == 0) write_result<D>(a, head, g, c, r);
     }
 }
@@ -987,7 +1012,7 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     // join; shares of few heads are many parts, which one team joins 32 at a time and 32 elements at once.
     // Equal shares of everything, or one or more clusters for each head: by the time that each takes in nanoseconds, for the lengths that the tables have room
     // for.  HBM gives 6500 bytes in one; an SM takes 60, of 4-bit blocks 38 (it computes for longer).  One cluster for a head needs no counters
-    // and no second join; shares of few heads are many parts, which one team joins, 128 elements at once and eight parts on their way.  Clusters of 4 and 8
+    // and no second join; shares of few heads are many parts, which one team joins, 128 elements at once and four parts on their way.  Clusters of 4 and 8
     // leave SMs of a GPC over.  (B8 H8/8 n8192 d128 bf16: clusters of four 43 us, shares 48; B1 H8/1 n131072 4 bits: 15 clusters of eight 15 us, one
     // cluster 60, shares 92; B64 H32/8 of 4000 keys 4 bits: shares 78, clusters do not fit.)
     const int heads = p.B * p.pool.Hkv, slots = C::kCtas * sms, units = (int)(((long long)p.max_pages * p.pool.page + C::kUnitKeys - 1) / C::kUnitKeys);
@@ -995,7 +1020,7 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     const double hbm = kUnitBytes * units * heads / 6500.0;
     auto stream = [&](double units_of_a_team, double teams_on_an_sm) { return std::max(hbm, std::ceil(units_of_a_team) * kUnitBytes * teams_on_an_sm / kSmRate); };
     const double equal = std::max(1.0, (double)units * heads / (C::kShares * sms)), parts = std::min((double)units, std::max(1.0, (double)C::kShares * sms / heads));
-    double best = stream(equal, C::kShares) + 2500.0 + 700.0 * std::ceil(parts / 8.0) * ((G * (D / 4) + 127) / 128);
+    double best = stream(equal, C::kShares) + 2500.0 + 700.0 * std::ceil(parts / 4.0) * ((G * (D / 4) + 127) / 128);
     int cl = 0, nc = 0;
     for (int c = 1; c <= 8; c *= 2) {
         const long long at_once = slots * (c == 8 ? 85LL : c == 4 ? 90LL : 100LL) / (100LL * c);
