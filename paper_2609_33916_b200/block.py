@@ -11,7 +11,11 @@ With `packed_qkv` (the default) the three projections are one GEMM against the s
 explicit strides (MOA_LAYOUT_STRIDED, no copy), dQ, dK, dV come back into one such array, and the backward of the
 projection is one GEMM for dh1 and one for dWqkv.  That form's 6 + 8 calls are made by the library (moa_block_fwd,
 moa_block_bwd: one call per direction from here) as long as the block's descriptors (nd, ad, md) are the ones it was built with; with
-changed ones (another dq_mode, say), and without `packed_qkv`, the calls (8 and 12) are made here."""
+changed ones (another dq_mode, say), without `packed_qkv`, and with rotary positions, the calls (8 and 12, one more with positions) are made here.
+
+With `rope` (inv_freq, a float32 tensor of d_rot / 2 on the device, or a dict of inv_freq, layout and factor) q and k are turned in place behind the
+projection, each token by its place in its sequence (self.pos, int32 [T], which may be replaced), and their gradients are turned back in front of the
+projection's backward pass."""
 from __future__ import annotations
 
 import math
@@ -23,7 +27,7 @@ WEIGHTS = ("g1", "g2", "Wq", "Wk", "Wv", "Wo", "W1", "W3", "W2")
 
 class TransformerBlock:
     def __init__(self, torch, B: int, n: int, H: int, d: int, d_ff: int, causal: bool, eps: float = 1e-5,
-                 packed_qkv: bool = True):
+                 packed_qkv: bool = True, rope=None):
         self.torch, self.B, self.n, self.H, self.d, self.d_ff, self.causal, self.eps = torch, B, n, H, d, d_ff, causal, eps
         self.packed = bool(packed_qkv)
         T, dm = B * n, H * d
@@ -39,6 +43,15 @@ class TransformerBlock:
                                    strides=(third, third, (dm, d, n * dm)))
         else:
             self.ad = mb.make_desc(B, H, n, d, causal, 1.0 / math.sqrt(d), layout=mb.MOA_LAYOUT_BNHD)
+        self.rope = rope if rope is None or isinstance(rope, dict) else {"inv_freq": rope}
+        if self.rope is not None:
+            inv = self.rope["inv_freq"]
+            if inv.dtype != torch.float32 or not inv.is_cuda or inv.dim() != 1 or not inv.is_contiguous():
+                raise ValueError("rope: inv_freq must be a contiguous float32 vector on the device")
+            row = 3 * dm if self.packed else dm
+            self.rd = mb.make_rope_desc(T, H, H, d, 2 * inv.numel(), self.rope.get("layout", mb.MOA_ROPE_HALF),
+                                        self.rope.get("factor", 1.0), q_stride=(row, d), k_stride=(row, d), q_out_stride=(row, d), k_out_stride=(row, d))
+            self.pos = torch.arange(n, dtype=torch.int32, device="cuda").repeat(B)
         self.md = mb.make_mlp_desc(T, dm, d_ff)
         self.bd = mb.moa_block_desc(B, n, H, d, d_ff, int(bool(causal)), eps, 1.0 / math.sqrt(d))
         self.proj = mb.make_gemm_desc(T, dm, dm)              # y = x W^T
@@ -100,7 +113,7 @@ class TransformerBlock:
             self.gqkv, g["Wo"], g["W1"], g["W3"], g["W2"], nws, aws, mws, nws.nbytes, aws.nbytes, mws.nbytes))
 
     def forward(self, x, w, stream=None):
-        if self.packed and self._descriptors() == self._built_with:
+        if self.packed and self.rope is None and self._descriptors() == self._built_with:
             mb.moa_block_fwd(self.bd, self._arrays(x, w, None), stream)
             return self.y
         s = stream
@@ -111,6 +124,8 @@ class TransformerBlock:
             mb.moa_gemm(self.proj, self.h1, w["Wq"], self.q, stream=s)
             mb.moa_gemm(self.proj, self.h1, w["Wk"], self.k, stream=s)
             mb.moa_gemm(self.proj, self.h1, w["Wv"], self.v, stream=s)
+        if self.rope is not None:
+            mb.moa_rope_fwd(self.rd, self.pos, self.rope["inv_freq"], self.q, self.k, self.q, self.k, s)
         mb.moa_attn_fwd(self.ad, self.q, self.k, self.v, self.o, self.L, self.aws, s)
         mb.moa_gemm(self.proj, self.o, w["Wo"], self.x2, R=x, stream=s)
         mb.moa_rmsnorm_fwd(self.nd, self.x2, w["g2"], self.h2, self.r2, s)
@@ -119,7 +134,7 @@ class TransformerBlock:
 
     def backward(self, x, w, dy, stream=None):
         s, g = stream, self.grads
-        if self.packed and self._descriptors() == self._built_with:
+        if self.packed and self.rope is None and self._descriptors() == self._built_with:
             mb.moa_block_bwd(self.bd, self._arrays(x, w, dy), s)
             return self.dx, g
         mb.moa_gated_mlp_bwd(self.md, self.h2, w["W1"], w["W3"], w["W2"], self.a, self.u, self.h, dy, self.dh2,
@@ -128,6 +143,8 @@ class TransformerBlock:
         mb.moa_gemm(self.wgrad, self.dx2, self.o, g["Wo"], stream=s)
         mb.moa_gemm(self.back, self.dx2, w["Wo"], self.do, stream=s)
         mb.moa_attn_bwd(self.ad, self.q, self.k, self.v, self.o, self.L, self.do, self.dq, self.dk, self.dv, self.aws, s)
+        if self.rope is not None:
+            mb.moa_rope_bwd(self.rd, self.pos, self.rope["inv_freq"], self.dq, self.dk, self.dq, self.dk, s)
         if self.packed:
             mb.moa_gemm(self.back3, self.dqkv, w["Wqkv"], self.dh1, stream=s)
             mb.moa_gemm(self.wgrad3, self.dqkv, self.h1, self.gqkv, stream=s)
