@@ -18,7 +18,8 @@
 // equal shares, one per resident team, on the device (the host does not know the lengths): every CTA adds up the lengths and finds its
 // teams' shares.  A head that lies in one share is written at once; the teams of the others leave partial results (at most two each), and the last of
 // them to come joins them, told by a counter that a one-block kernel in front has cleared; the streaming starts without waiting for that.
-// Where there are few heads, a cluster takes each and joins its teams through distributed shared memory.
+// Where there are few heads, one or more clusters take each and join their teams through distributed shared memory (several: the last of them to come
+// joins what the others left).  Which of the two: by the estimate in `launch`.
 #include "cache_layout.cuh"
 #include "ptx.cuh"
 #include <algorithm>
@@ -624,12 +625,16 @@ __device__ __forceinline__ void last_joins(const PagedArgs &a, int team, int hea
 {
     constexpr int kJoin = 32 * kWarps, kBatch = 4;
     const int tid = threadIdx.x % kJoin;
-    __threadfence();                            // (this thread's part, before the count)
+    // the fences of the thread that counts order what the barriers in front of and behind it have gathered: the team's part before the count, the
+    // other teams' parts, if it is the last, before the reads
     named_barrier(1 + team, kJoin);
-    if (tid == 0) *flag = atomicAdd(a.counters + ca, 1u);
+    if (tid == 0) {
+        __threadfence();
+        *flag = atomicAdd(a.counters + ca, 1u);
+        __threadfence();
+    }
     named_barrier(1 + team, kJoin);
     if (*flag != (unsigned)(cb - ca)) return;
-    __threadfence();
     for (int idx = tid; idx < a.G * (D / 4); idx += kJoin) {
         const int g = idx / (D / 4), c = 4 * (idx % (D / 4));
         float mt = -INFINITY, ls = 0.f;
@@ -764,12 +769,15 @@ __device__ __forceinline__ void finish_clusters(const PagedArgs &a, uint8_t *sha
 {
     cluster_sync_all();
     if (tid >= 0) combine<D, kInt4, NQ>(a, shared, tid, threads);
-    if (a.nc > 1) __threadfence();                             // (this thread's part, before the count)
     __syncwarp();
     cluster_sync_all();                                        // nobody leaves while another CTA may still read its shared memory
     if (a.nc == 1) return;
     const int head = (int)blockIdx.x / (a.cl * a.nc), rank = (int)cluster_ctarank();
-    if (tid == 0 && rank == 0) *flag = atomicAdd(a.counters + head, 1u);
+    if (tid == 0 && rank == 0) {                               // (the fences: as in last_joins)
+        __threadfence();
+        *flag = atomicAdd(a.counters + head, 1u);
+        __threadfence();
+    }
     __syncwarp();
     cluster_sync_all();
     unsigned int came;
@@ -777,7 +785,6 @@ __device__ __forceinline__ void finish_clusters(const PagedArgs &a, uint8_t *sha
     __syncwarp();
     cluster_sync_all();
     if (tid < 0 || came != (unsigned)(a.nc - 1)) return;
-    __threadfence();
     const int all = a.G * (D / 4), first = all * rank / a.cl, last = all * (rank + 1) / a.cl;
     for (int i0 = first; i0 < last; i0 += threads / 4) {       // (whole warps: the exchanges)
         const int idx = i0 + tid / 4, at = min(idx, last - 1), g = at / (D / 4), c = 4 * (at % (D / 4));
@@ -1007,9 +1014,6 @@ cudaError_t launch(const PagedProblem &p, const void *q, const void *pool, const
     constexpr auto kernel = [] { if constexpr (kInt4) return paged_decode4_kernel<D, NQ, false>; else return paged_decode16_kernel<D, NQ, false>; }();
     constexpr auto clusters = [] { if constexpr (kInt4) return paged_decode4_kernel<D, NQ, true>; else return paged_decode16_kernel<D, NQ, true>; }();
     const int G = p.H / p.pool.Hkv, sms = device_info().sms, shares = shares_for(p, C::kShares, C::kUnitKeys), most = 4 * sms;
-    // One or more clusters for each head, or equal shares of everything.  Clusters that run at once: those of 4 and 8 leave SMs of a GPC over.  In
-    // nanoseconds, for the lengths that the tables have room for: an SM streams about 40 bytes in one; one cluster for a head needs no counters and no second
-    // join; shares of few heads are many parts, which one team joins 32 at a time and 32 elements at once.
     // Equal shares of everything, or one or more clusters for each head: by the time that each takes in nanoseconds, for the lengths that the tables have room
     // for.  HBM gives 6500 bytes in one; an SM takes 60, of 4-bit blocks 38 (it computes for longer).  One cluster for a head needs no counters
     // and no second join; shares of few heads are many parts, which one team joins, 128 elements at once and four parts on their way.  Clusters of 4 and 8
