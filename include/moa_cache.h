@@ -79,8 +79,8 @@ moa_status moa_kv_gather(const moa_gather_desc *desc, const void *pool, const in
  * the end of a sequence does not count.
  * q: B x H x d, strides {sequence, head} as above; out [B,H,d]; lse [B,H] fp32 natural-log logsumexp of the scaled scores, may be NULL;
  * table int32, rows of max_pages entries, table_stride entries apart (0: max_pages); lens [B] int32.  dtype of q, out:
- * MOA_BF16 (fp32 scores, statistics and sums; the weights, and with 4 bits their products with V's scales, are rounded to bf16 for the second
- * product).  |scale| <= 2^60.  A page of 4 bits wants |q| < 2^59 and |v| < 2^55, and values below 2^-80 may come out as 0 (its codes are used as numbers at
+ * MOA_BF16 (fp32 scores, statistics and sums; the weights, with 4 bits their products with V's scales, are rounded once to bf16 for the
+ * second product).  |scale| <= 2^60.  A page of 4 bits wants |q| < 2^59 and |v| < 2^55, and values below 2^-80 may come out as 0 (its codes are used as numbers at
  * the low end of bf16, against operands raised by up to 2^68).  A score that is NaN makes its row NaN.  Lengths are read on the device only: a captured call serves growing sequences.
  * Workspace: moa_paged_decode_workspace_bytes (partial results of sequences that several CTAs share); two calls that may
  * overlap need two. */

@@ -8,7 +8,9 @@
 // bytes is its instructions: an SM has about 400 issue slots in the time HBM takes for 16 keys of a head at d = 128 (2304 bytes).  So
 //   * codes become bf16 by one mask (see `nibbles`).  K: the 8 too many are taken off in the products' starting value, -8 sum(q) of the
 //     group; V: by one packed subtraction, exact;
-//   * K's scale multiplies the products of a group of 32, in fp32; V's is multiplied into the weights (bf16, as the weights of the products are);
+//   * K's scale multiplies the products of a group of 32, in fp32; V's is multiplied into the weights, and the product rounded to bf16: the one rounding
+//     of a weight, as in the bf16 form (a weight goes there in two pieces; rounded before, too, the results are off by 0.0029 in place of 0.0023, and
+//     the largest case takes 233 us in place of 241);
 //   * the page's layout (cache_layout.cuh) is the one in which a lane's codes and scales are 16-byte words: no exchange of any kind.
 // Loads.  4 bits: a fifth warp asks for the blocks of a unit by bulk copies, a lane for each of its eight blocks, with the table entries of the next four
 // units in its lanes and those behind them on their way; a ring of three units.  bf16: a warp streams its 16 keys at a time through a
@@ -136,7 +138,15 @@ __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b)
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
+__device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
 __device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ uint32_t upper(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632); }      // their upper halves
+__device__ __forceinline__ float rest(float a) { return a - __uint_as_float(__float_as_uint(a) & 0xffff0000u); }
 __device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 template <int kUnitKeys> __device__ __forceinline__ int units_of(int len) { return len > 0 ? (len + kUnitKeys - 1) / kUnitKeys : 1; }
@@ -348,7 +358,7 @@ struct HeadState {
     }
 
     // O^T += V^T P^T of a block; keys of it from `in` on do not count (their weights are 0; their scales may not be numbers)
-    __device__ __forceinline__ void values(const uint32_t (&pb)[NQ][2], uint32_t blk, int lane, bool ragged, int in)
+    __device__ __forceinline__ void values(const uint32_t (&pb)[NQ][2], const uint32_t (&pr)[NQ][2], uint32_t blk, int lane, bool ragged, int in)
     {
         const int t4 = lane % 4;
         if constexpr (kInt4) {
@@ -378,7 +388,10 @@ struct HeadState {
                 const uint32_t w01 = __byte_perm(va[y / 2][0], va[y / 2][1], sel), w23 = __byte_perm(va[y / 2][2], va[y / 2][3], sel);
                 uint32_t b0[NQ], b1[NQ];
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) { b0[n] = mul2(pb[n][0], vs[y][0]); b1[n] = mul2(pb[n][1], vs[y][1]); }
+                for (int n = 0; n < NQ; ++n) {
+                    b0[n] = fma2(pb[n][0], vs[y][0], mul2(pr[n][0], vs[y][0]));
+                    b1[n] = fma2(pb[n][1], vs[y][1], mul2(pr[n][1], vs[y][1]));
+                }
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const uint32_t x01 = u ? w01 >> 8 : w01, x23 = u ? w23 >> 8 : w23;
@@ -457,7 +470,8 @@ struct HeadState {
                     }
                 }
         }
-        uint32_t pb[kSub][NQ][2];
+        // 4 bits: a weight as its upper half and what that leaves, so that its product with V's scale is rounded once
+        uint32_t pb[kSub][NQ][2], pr[kSub][NQ][2];
 #pragma unroll
         for (int s = 0; s < kSub; ++s)
 #pragma unroll
@@ -466,11 +480,18 @@ struct HeadState {
                 const float p2 = ex2(fmaf(sc[s][n][2], scale, -ref[n][0])), p3 = ex2(fmaf(sc[s][n][3], scale, -ref[n][1]));
                 l[n][0] += p0 + p2;
                 l[n][1] += p1 + p3;
-                pb[s][n][0] = transpose8(pack_bf16(p0, p1));
-                pb[s][n][1] = transpose8(pack_bf16(p2, p3));
+                if constexpr (kInt4) {
+                    pb[s][n][0] = transpose8(upper(p0, p1));
+                    pb[s][n][1] = transpose8(upper(p2, p3));
+                    pr[s][n][0] = transpose8(pack_bf16(rest(p0), rest(p1)));
+                    pr[s][n][1] = transpose8(pack_bf16(rest(p2), rest(p3)));
+                } else {
+                    pb[s][n][0] = transpose8(pack_bf16(p0, p1));
+                    pb[s][n][1] = transpose8(pack_bf16(p2, p3));
+                }
             }
 #pragma unroll
-        for (int s = 0; s < kSub; ++s) values(pb[s], st + s * kBlock, lane, ragged, here >> s & 1 ? left - 16 * s : 0);
+        for (int s = 0; s < kSub; ++s) values(pb[s], pr[s], st + s * kBlock, lane, ragged, here >> s & 1 ? left - 16 * s : 0);
     }
 
     // Eight queries (the n-th eight) of this warp into the merge: rows of kLd floats, and (maximum, sum) of each
