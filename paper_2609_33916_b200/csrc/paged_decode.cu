@@ -73,6 +73,7 @@ struct Cfg {
     static constexpr int kTeam = (offFlag + 4 + 127) / 128 * 128;
     static constexpr int offScan = kTeams * kTeam;                                     // of the CTA: 16 words of sums, two for each team
     static constexpr int kTotal = offScan + 128;
+    static_assert(kCtas * (kTotal + 1024) <= 228 * 1024, "an SM holds kCtas of them, with 1 KB of the system's each (bf16, d = 128: to the byte; one CTA 165 us, two 160)");
     static constexpr int kNO = D / 16;                                                 // tiles of O^T
 };
 
