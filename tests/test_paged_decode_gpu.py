@@ -1,9 +1,9 @@
 """Decode attention over pages against the 64-bit oracle.
 
-Tolerance of an element, with A = sum_j p_j |v_j| of its column: the weights are rounded to bf16 (2^-8 of each), in the 4-bit form once more when they
-meet the scale, and the result is rounded to bf16: (1 or 2) 2^-8 A + 2^-8 |o|.  Scores: products are exact, and are summed in 32 bits; a sum of N
-terms, each addition cut to 24 bits, is within N 2^-23 sum |terms|, in the 4-bit form of 34 terms of up to 143 |q| s per group (the
-codes carry 128 and start from -136): e = scale 34 2^-23 (143 + 136) s sum|q|, in the bf16 form e = scale 128 2^-23 sum |q k|.  A score that is off by e
+Tolerance of an element, with A = sum_j p_j |v_j| of its column: the weights are rounded to bf16 (2^-8 of each; the 4-bit form may round once more where
+they meet the scale), and the result is rounded to bf16: (1 or 2) 2^-8 A + 2^-8 |o|.  Scores: products are exact, and are summed in 32 bits; a sum of N
+terms, each addition cut to 24 bits, is within N 2^-23 sum |terms|, in the 4-bit form of 34 terms of up to 143 |q| s per group (room for
+codes that carry 128 and start from -136; those of the kernel are 1 to 15 and start from -8): e = scale 34 2^-23 (143 + 136) s sum|q|, in the bf16 form e = scale 128 2^-23 sum |q k|.  A score that is off by e
 takes the weights off by a factor within 1 +- 2 e and lse by e.  fp32 sums of the weights and of the products: 1e-5."""
 import numpy as np
 import pytest
