@@ -47,13 +47,11 @@ __device__ __forceinline__ float round_bf16(double v)
     return (float)__longlong_as_double(b);
 }
 
-// A rotated pair, f (x1 cos - x2 sin) and f (x2 cos + x1 sin), in 64 bits and rounded to bf16.  The angle is reduced to a part of a turn as a sum of two
-// doubles (1 / (2 pi) has its second part here), so that positions of millions lose nothing.
+// A rotated pair, f (x1 cos - x2 sin) and f (x2 cos + x1 sin), in 64 bits and rounded to bf16.
 __device__ __noinline__ float2 exact_turn(float x1, float x2, int pos, float f, float factor)
 {
-    const double a = (double)pos * (double)f, h = a * 0x1.45f306dc9c883p-3, l = fma(a, 0x1.45f306dc9c883p-3, -h) + a * -0x1.6b01ec5417056p-57;
     double s, c;
-    sincospi(2.0 * ((h - rint(h)) + l), &s, &c);
+    sincospi(2.0 * part_of_turn(pos, f), &s, &c);
     c *= (double)factor;
     s *= (double)factor;
     return make_float2(round_bf16((double)x1 * c - (double)x2 * s), round_bf16((double)x2 * c + (double)x1 * s));

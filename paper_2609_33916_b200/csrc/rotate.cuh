@@ -25,13 +25,19 @@ struct FastDiv {
     }
 };
 
-// cos and sin of pos * f.  The product has 55 bits at most and a double 53; it is reduced to a part of a turn there, so that an angle of
-// a million radians is as exact as one of one.  What rounding the part to 32 bits takes off goes back in by the first term of the series:
-// both results are within 1.5 * 2^-24.
+// pos * f, rounded to 64 bits (55 would be exact), as a part of a turn: 1 / (2 pi) in two parts, and what the product with the first one is rounded by, so
+// that the farthest position loses nothing either (with one double for all of it, 2^31 radians were off by 5 * 2^-24)
+__device__ __forceinline__ double part_of_turn(int pos, float f)
+{
+    const double a = (double)pos * (double)f, h = a * 0x1.45f306dc9c883p-3, l = fma(a, 0x1.45f306dc9c883p-3, -h) + a * -0x1.6b01ec5417056p-57;
+    return (h - rint(h)) + l;
+}
+
+// cos and sin of pos * f, the product rounded to 64 bits.  What rounding the part of a turn to 32 bits takes off goes back in by the first term of the
+// series: both results are within 1.5 * 2^-24.
 __device__ __forceinline__ float2 position_angle(int pos, float f)
 {
-    double t = (double)pos * (double)f * 0.15915494309189533577;      // 1 / (2 pi)
-    t -= rint(t);
+    const double t = part_of_turn(pos, f);
     const float h = (float)t, l = 6.2831853071795864769f * (float)(t - (double)h);
     float s, c;
     sincospif(2.f * h, &s, &c);
