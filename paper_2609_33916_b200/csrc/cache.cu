@@ -4,8 +4,8 @@
 // tokens with all their rows (queries, keys, values), the angles of a token are made once and shared through shared memory, and a row is d / 16
 // lanes with two 16-byte pieces each, several rows in flight per lane.
 //
-// K is rounded to the nearest bf16 of the exact rotation.  In 32 bits the rotation is within 4.5 * 2^-24 f (|x1| + |x2|) of it (cosine and sine 1.5, the
-// factor, a product and the sum one each); where the two ends of that interval round apart, one element in about 5000, it is made again in 64 bits.
+// K is rounded to the nearest bf16 of the exact rotation, subnormal ones included.  In 32 bits the rotation is within 4.5 * 2^-24 f (|x1| + |x2|) of it (cosine
+// and sine 1.5, the factor, a product and the sum one each), and 2^-147; where the two ends of that interval round apart, one element in about 5000, it is made again in 64 bits.
 // So what a key quantises to does not depend on which arithmetic turned it, and a 4-bit page is a function of the bf16 page's bits.
 //
 // Quantising: 32 neighbours share a scale s = bf16(amax / 7); x / s with one correction by the remainder is exact wherever the quotient is a tie
@@ -37,14 +37,15 @@ struct AppendArgs {
     float factor;
 };
 
-// The nearest bf16 of a double, in one rounding (half to even on the 45 bits that go); by way of float where the result has no normal bf16.
+// The nearest bf16 of a double, in one rounding: half to even on the 45 bits that go, or, where bf16 is subnormal, by a sum whose last place is its step.
 __device__ __forceinline__ float round_bf16(double v)
 {
     const double a = fabs(v);
-    if (!(a >= 0x1p-126 && a < 0x1.fep127)) return __bfloat162float(__float2bfloat16_rn((float)v));
+    if (a < 0x1p-126) return (float)copysign((a + 0x1.8p-81) - 0x1.8p-81, v);
+    if (!(a < INFINITY)) return (float)v;
     long long b = __double_as_longlong(v);
     b = (b + ((1LL << 44) - 1) + ((b >> 45) & 1)) & ~((1LL << 45) - 1);
-    return (float)__longlong_as_double(b);
+    return (float)__longlong_as_double(b);      // (2^128 and above: infinity)
 }
 
 // A rotated pair, f (x1 cos - x2 sin) and f (x2 cos + x1 sin), in 64 bits and rounded to bf16.
@@ -146,11 +147,14 @@ __device__ __forceinline__ void turn_key(Piece &x, Piece &y, const float (&c)[8]
     const uint4 xi = x.w, yi = y.w;
     x.unpack(fx);
     y.unpack(fy);
-    const float off = 2.8e-7f * fabsf(factor);
+    const float f1 = fmaxf(fabsf(factor), 0x1p-100f);      // (below, the factor's products are not within 2^-24)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float x1 = kPairs ? (i < 4 ? fx[2 * i] : fy[2 * i - 8]) : fx[i], x2 = kPairs ? (i < 4 ? fx[2 * i + 1] : fy[2 * i - 7]) : fy[i];
-        e[i] = off * (fabsf(x1) + fabsf(x2));
+        // (what a part of the rotation may overflow with, this product does: then the pair is in doubt.  Where results are subnormal, each of three
+        // roundings is off by 2^-150 whatever the size: 2^-147, unless both elements are 0)
+        const float size = f1 * (fabsf(x1) + fabsf(x2));
+        e[i] = fmaxf(2.8e-7f * size, fminf(size, 0x1p-147f));
     }
     rotate<8, kPairs>(fx, fy, c, s);
     uint32_t doubt = 0;
