@@ -80,8 +80,9 @@ moa_status moa_kv_gather(const moa_gather_desc *desc, const void *pool, const in
  * q: B x H x d, strides {sequence, head} as above; out [B,H,d]; lse [B,H] fp32 natural-log logsumexp of the scaled scores, may be NULL;
  * table int32, rows of max_pages entries, table_stride entries apart (0: max_pages); lens [B] int32.  dtype of q, out:
  * MOA_BF16 (fp32 scores, statistics and sums; the weights, with 4 bits their products with V's scales, are rounded once to bf16 for the
- * second product).  |scale| <= 2^60.  A page of 4 bits wants |q| < 2^59 and |v| < 2^55, and values below 2^-80 may come out as 0 (its codes are used as numbers at
- * the low end of bf16, against operands raised by up to 2^68).  A score that is NaN makes its row NaN.  Lengths are read on the device only: a captured call serves growing sequences.
+ * second product).  |scale| <= 2^60.  A page of 4 bits wants |q| < 2^59 and |v| < 2^55.  Its codes are used as numbers at the low end of bf16, against operands raised by up to
+ * 2^68, so fp32's last place lies higher there: a query's product with the codes of a group is kept to 2^-84 (times the group's scale), a result's sum over 16 keys to
+ * 2^-80; results below 2^-57 have fewer bits than bf16, those below 2^-80 may be 0.  A score that is NaN makes its row NaN.  Lengths are read on the device only: a captured call serves growing sequences.
  * Workspace: moa_paged_decode_workspace_bytes (partial results of sequences that several CTAs share); two calls that may
  * overlap need two. */
 typedef struct {

@@ -23,6 +23,8 @@ NVCC_FLAGS = [
 ]
 # the fp32 SIMT path is held to 1e-5 against the fp64 oracle, the rotations and the cache's codes to the nearest value: no fast-math there
 NO_FAST_MATH = {"simt_kernels.cu", "rope.cu", "cache.cu"}
+# 4-bit codes are used as numbers at the low end of bf16, and what they are multiplied into lies near the low end of fp32: its small numbers are kept
+KEEPS_SMALL = {"paged_decode.cu"}
 
 
 def _nvcc() -> str:
@@ -53,7 +55,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
         obj = os.path.join(OBJ, os.path.basename(src)[:-3] + ".o")
         objs.append(obj)
         if force or _stale(obj, [src] + headers):
-            flags = [f for f in NVCC_FLAGS if not (f == "--use_fast_math" and os.path.basename(src) in NO_FAST_MATH)]
+            name = os.path.basename(src)
+            flags = [f for f in NVCC_FLAGS if not (f == "--use_fast_math" and name in NO_FAST_MATH | KEEPS_SMALL)]
+            if name in KEEPS_SMALL:
+                flags = flags + ["-prec-div=false", "-prec-sqrt=false"]
             if verbose:
                 flags = flags + ["-Xptxas", "-v"]
             jobs.append([_nvcc()] + flags + ["-c", src, "-o", obj])

@@ -123,7 +123,9 @@ __device__ __forceinline__ void mma16816_from(float (&d)[4], const uint32_t (&a)
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
 }
 // Codes as numbers where they lie: a nibble at bits 0..3 or 4..7 of a bf16 whose other bits are zero is c * 2^-133 or c * 2^-129 (the format is
-// linear from 0 to twice its least normal number), so one mask makes a pair of them.  What they meet is larger by 2^64.
+// linear from 0 to twice its least normal number), so one mask makes a pair of them.  What they meet is larger by 2^64: sums of values are 2^-69 or 2^-65 of
+// what they stand for and reach into fp32's subnormal numbers, which this file keeps (it is built without flushing them; the same time, and without
+// it half of the results below 2^-57 were 0).
 constexpr int kCodeExp0 = -133, kCodeExp1 = -129, kLift = 64;
 __device__ __forceinline__ uint32_t nibbles(uint32_t w, int i) { return w & (i & 1 ? 0x00f000f0u : 0x000f000fu); }      // w: shifted by 8 for i = 2, 3
 __host__ __device__ constexpr float exp2i(int e) { return e < 0 ? 0.5f * exp2i(e + 1) : e > 0 ? 2.f * exp2i(e - 1) : 1.f; }
@@ -566,7 +568,7 @@ __device__ __forceinline__ void join(const PagedArgs &a, const HeadState<D, kInt
                 const size_t at = (size_t)head * a.G + 8 * n + r;
                 const float inv = ls == 0.f ? 0.f : 1.f / ls;
                 *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
-                if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + log2f(ls)) * kLn2;
+                if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + __log2f(ls)) * kLn2;
             } else {
                 const size_t at = (size_t)slot * a.G + 8 * n + r;
                 *reinterpret_cast<float4 *>(a.part_o + at * D + c) = ot;
@@ -638,7 +640,7 @@ __device__ __forceinline__ void write_result(const PagedArgs &a, int head, int g
     const size_t at = (size_t)head * a.G + g;
     const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
     *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(r.o.x * inv, r.o.y * inv), pack_bf16(r.o.z * inv, r.o.w * inv));
-    if (a.lse && c == 0) a.lse[at] = r.l == 0.f ? -INFINITY : (r.m + log2f(r.l)) * kLn2;
+    if (a.lse && c == 0) a.lse[at] = r.l == 0.f ? -INFINITY : (r.m + __log2f(r.l)) * kLn2;
 }
 
 // A head that lies in several shares, ca to cb: the team that leaves its part last joins them all (nobody waits for anyone).
@@ -688,7 +690,7 @@ __device__ __forceinline__ void last_joins(const PagedArgs &a, int team, int hea
         const size_t at = (size_t)head * a.G + g;
         const float inv = ls == 0.f ? 0.f : 1.f / ls;
         *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
-        if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + log2f(ls)) * kLn2;
+        if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + __log2f(ls)) * kLn2;
     }
 }
 
