@@ -14,11 +14,13 @@ moa_block_bwd: one call per direction from here) as long as the block's descript
 changed ones (another dq_mode, say), without `packed_qkv`, and with rotary positions, the calls (8 and 12, one more with positions) are made here.
 
 With `rope` (inv_freq, a float32 tensor of d_rot / 2 on the device, or a dict of inv_freq, layout and factor) q and k are turned in place behind the
-projection, each token by its place in its sequence (self.pos, int32 [T], which may be replaced), and their gradients are turned back in front of the
-projection's backward pass."""
+projection, each token by its place in its sequence, and their gradients are turned back in front of the projection's backward pass.  self.pos, int32 [T] on
+the device, holds the places: it may be replaced, or written to between a backward pass and the next forward pass (a backward pass turns back by the
+tensor that its forward pass turned by)."""
 from __future__ import annotations
 
 import math
+from types import MappingProxyType
 
 from . import binding as mb
 
@@ -43,15 +45,18 @@ class TransformerBlock:
                                    strides=(third, third, (dm, d, n * dm)))
         else:
             self.ad = mb.make_desc(B, H, n, d, causal, 1.0 / math.sqrt(d), layout=mb.MOA_LAYOUT_BNHD)
-        self.rope = rope if rope is None or isinstance(rope, dict) else {"inv_freq": rope}
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        # (read-only: the descriptor below says how many frequencies there are)
+        self.rope = rope if rope is None else MappingProxyType(dict(rope) if isinstance(rope, dict) else {"inv_freq": rope})
         if self.rope is not None:
             inv = self.rope["inv_freq"]
-            if inv.dtype != torch.float32 or not inv.is_cuda or inv.dim() != 1 or not inv.is_contiguous():
-                raise ValueError("rope: inv_freq must be a contiguous float32 vector on the device")
+            if inv.dtype != torch.float32 or inv.device != self.device or inv.dim() != 1 or not inv.is_contiguous():
+                raise ValueError("rope: inv_freq must be a contiguous float32 vector on the block's device")
             row = 3 * dm if self.packed else dm
             self.rd = mb.make_rope_desc(T, H, H, d, 2 * inv.numel(), self.rope.get("layout", mb.MOA_ROPE_HALF),
                                         self.rope.get("factor", 1.0), q_stride=(row, d), k_stride=(row, d), q_out_stride=(row, d), k_out_stride=(row, d))
-            self.pos = torch.arange(n, dtype=torch.int32, device="cuda").repeat(B)
+            self.pos = torch.arange(n, dtype=torch.int32, device=self.device).repeat(B)
+            self._turned_by = self.pos                        # positions of the last forward pass
         self.md = mb.make_mlp_desc(T, dm, d_ff)
         self.bd = mb.moa_block_desc(B, n, H, d, d_ff, int(bool(causal)), eps, 1.0 / math.sqrt(d))
         self.proj = mb.make_gemm_desc(T, dm, dm)              # y = x W^T
@@ -84,6 +89,20 @@ class TransformerBlock:
         self.grads = dict(g1=E(dm), g2=E(dm), Wq=gqkv[:dm], Wk=gqkv[dm:2 * dm], Wv=gqkv[2 * dm:], Wo=E(dm, dm),
                           W1=E(d_ff, dm), W3=E(d_ff, dm), W2=E(dm, d_ff))
         self.gqkv = gqkv
+
+    @property
+    def pos(self):
+        """Positions of the tokens, int32 [T] (blocks with `rope`)."""
+        return self._pos
+
+    @pos.setter
+    def pos(self, pos):
+        if self.rope is None:
+            raise ValueError("a block without rope has no positions")
+        if (not isinstance(pos, self.torch.Tensor) or pos.dtype != self.torch.int32 or pos.device != self.device or tuple(pos.shape) != (self.T,)
+                or not pos.is_contiguous()):
+            raise ValueError(f"pos must be a contiguous int32 vector of {self.T} positions on the block's device")
+        self._pos = pos
 
     def prepare_weights(self, w: dict) -> dict:
         """The weights as the block reads them: with packed_qkv, adds Wqkv = [Wq; Wk; Wv] (a choice of parameter
@@ -125,7 +144,8 @@ class TransformerBlock:
             mb.moa_gemm(self.proj, self.h1, w["Wk"], self.k, stream=s)
             mb.moa_gemm(self.proj, self.h1, w["Wv"], self.v, stream=s)
         if self.rope is not None:
-            mb.moa_rope_fwd(self.rd, self.pos, self.rope["inv_freq"], self.q, self.k, self.q, self.k, s)
+            self._turned_by = self.pos
+            mb.moa_rope_fwd(self.rd, self._turned_by, self.rope["inv_freq"], self.q, self.k, self.q, self.k, s)
         mb.moa_attn_fwd(self.ad, self.q, self.k, self.v, self.o, self.L, self.aws, s)
         mb.moa_gemm(self.proj, self.o, w["Wo"], self.x2, R=x, stream=s)
         mb.moa_rmsnorm_fwd(self.nd, self.x2, w["g2"], self.h2, self.r2, s)
@@ -144,7 +164,7 @@ class TransformerBlock:
         mb.moa_gemm(self.back, self.dx2, w["Wo"], self.do, stream=s)
         mb.moa_attn_bwd(self.ad, self.q, self.k, self.v, self.o, self.L, self.do, self.dq, self.dk, self.dv, self.aws, s)
         if self.rope is not None:
-            mb.moa_rope_bwd(self.rd, self.pos, self.rope["inv_freq"], self.dq, self.dk, self.dq, self.dk, s)
+            mb.moa_rope_bwd(self.rd, self._turned_by, self.rope["inv_freq"], self.dq, self.dk, self.dq, self.dk, s)
         if self.packed:
             mb.moa_gemm(self.back3, self.dqkv, w["Wqkv"], self.dh1, stream=s)
             mb.moa_gemm(self.wgrad3, self.dqkv, self.h1, self.gqkv, stream=s)
