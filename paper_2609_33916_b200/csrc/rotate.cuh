@@ -9,7 +9,8 @@ namespace moa {
 // x / d for x < 2^31, by a product: (x * mul) >> 32 >> shift (Granlund and Montgomery's round-up method, 33-bit multiplier kept as 32 bits + 1)
 struct FastDiv {
     uint32_t d, mul, shift;
-    explicit FastDiv(uint32_t div = 1) : d(div), mul(0), shift(0)
+    FastDiv() : FastDiv(1) {}
+    explicit FastDiv(uint32_t div) : d(div), mul(0), shift(0)
     {
         while ((1ull << shift) < div) ++shift;
         mul = (uint32_t)((((1ull << shift) - div) << 32) / div + 1);
