@@ -74,7 +74,6 @@ struct Cfg {
     static constexpr int offScan = kTeams * kTeam;                                     // of the CTA: 16 words of sums, two for each team
     static constexpr int kTotal = offScan + 128;
     static_assert(kCtas * (kTotal + 1024) <= 228 * 1024, "an SM holds kCtas of them, with 1 KB of the system's each (bf16, d = 128: to the byte; one CTA 165 us, two 160)");
-    static constexpr int kNO = D / 16;                                                 // tiles of O^T
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, int bytes)
@@ -707,24 +706,24 @@ __device__ __forceinline__ void walk(const PagedArgs &a, const Share &sh, Place<
         for (; done < count; ++done, ++use.t) next(s, use);
         cp_wait<0>();
         join<D, kInt4, NQ, true>(a, s, smem, team, 0, false, 0);
-        return;
-    }
-    while (done < count) {
-        const int first = use.t, steps = min(use.end - use.t, count - done), head = use.b * a.Hkv + use.h;
-        s.begin(a, q, use.b, use.h, lane);
-        for (int i = 0; i < steps; ++i, ++done, ++use.t) next(s, use);
-        const bool whole = first == 0 && use.t == use.end;
-        join<D, kInt4, NQ, false>(a, s, smem, team, head, whole, 2 * sh.c + (first == 0 ? 1 : 0));
-        if (!whole) {
-            // the head's first and last unit, and whose shares those are in
-            const int next_unit = sh.u0 + done;
-            last_joins<D, C>(a, team, head, first == 0 ? sh.c : share_of(sh, next_unit - use.t),
-                             use.t == use.end ? sh.c : share_of(sh, next_unit - use.t + use.end - 1), reinterpret_cast<unsigned int *>(smem + C::offFlag));
-        }
-        if (use.t == use.end) {
-            int b = use.b, h = use.h + 1;
-            if (h == a.Hkv) { h = 0; ++b; }
-            use.set(b, h, 0, b == use.b ? use.len : length_of(a, lens, b));
+    } else {
+        while (done < count) {
+            const int first = use.t, steps = min(use.end - use.t, count - done), head = use.b * a.Hkv + use.h;
+            s.begin(a, q, use.b, use.h, lane);
+            for (int i = 0; i < steps; ++i, ++done, ++use.t) next(s, use);
+            const bool whole = first == 0 && use.t == use.end;
+            join<D, kInt4, NQ, false>(a, s, smem, team, head, whole, 2 * sh.c + (first == 0 ? 1 : 0));
+            if (!whole) {
+                // the head's first and last unit, and whose shares those are in
+                const int next_unit = sh.u0 + done;
+                last_joins<D, C>(a, team, head, first == 0 ? sh.c : share_of(sh, next_unit - use.t),
+                                 use.t == use.end ? sh.c : share_of(sh, next_unit - use.t + use.end - 1), reinterpret_cast<unsigned int *>(smem + C::offFlag));
+            }
+            if (use.t == use.end) {
+                int b = use.b, h = use.h + 1;
+                if (h == a.Hkv) { h = 0; ++b; }
+                use.set(b, h, 0, b == use.b ? use.len : length_of(a, lens, b));
+            }
         }
     }
 }
