@@ -10,14 +10,15 @@ Of an element, with A = sum_j p_j |v_j| of its column and p the normalised weigh
             a factor within 1 +- 2 e, and lse by e.
   the rest  the argument of a weight's power is at most 128 in size and is rounded to 24 bits, 2^-18, the power itself is within 2^-22; sums of 2000 keys, 16 at once
             in each of four warps: 32 * 2^-23; joins: a few 2^-24: 1e-5 A together.
-Of all results together, as a part of |o|: a rounding of numbers whose logarithms are spread evenly is off by 2^-8 (0.541 / 3)^0.5 = 1.66e-3 of them in the mean
-square (half a step is 2^-8 / m at m in [1, 2), and the mean of m^-2 is 3 / (8 ln 2)).  Values of both signs: weights' errors add up as the results themselves do.
-Two roundings, the weight's or its product's and the result's, are 2.35e-3, three 2.87e-3: the bound is two and a half, 2.62e-3."""
+Of the results of many long rows together, each as a part of its norm: a rounding is off by 2^(e-8) / 3^0.5 in the mean square, where the number is m 2^e with m in
+[1, 2).  Where logarithms are spread evenly, the mean square of m is 3 / (2 ln 2), so of the numbers' own it is 2^-8 (2 ln 2 / 9)^0.5 = 1.53e-3.  Values of both
+signs: the weights' errors add up as the results themselves do.  Two roundings, the weight's or its product's and the result's, are 2.17e-3, three 2.66e-3: the bound
+lies between, at 2.45 of them, 2.40e-3, and holds rows of 500 keys and more, where there are 64 at least."""
 import numpy as np
 
 from oracle import cache as oc
 
-NORM = 2.5 ** 0.5 * 1.66e-3
+NORM = 2.45 ** 0.5 * 2.0 ** -8 * (2 * np.log(2) / 9) ** 0.5
 
 
 def check_paged(out, lse, q, K, V, table, lens, scale, four_bits, most_key, low=0.0, norm=True):
@@ -34,7 +35,8 @@ def check_paged(out, lse, q, K, V, table, lens, scale, four_bits, most_key, low=
     assert np.all(over <= 0), (float(np.nanmax(over / (mass + 1e-300))), np.argwhere(~(over <= 0))[:5])
     np.testing.assert_array_equal(lse[~fin], ref["lse"][~fin])
     assert np.all(np.abs(lse[fin] - ref["lse"][fin]) <= (e + 1e-5 * (1 + np.abs(np.where(fin, ref["lse"], 0.0))))[fin])
-    if norm:
-        far = float(np.linalg.norm(out - ref["o"]) / np.linalg.norm(ref["o"]))
-        assert far <= NORM, far
+    long = np.broadcast_to((np.asarray(lens) >= 500)[:, None], fin.shape) & fin
+    if norm and long.sum() >= 64:
+        far = np.linalg.norm(out - ref["o"], axis=-1)[long] / np.linalg.norm(ref["o"], axis=-1)[long]
+        assert np.sqrt(np.mean(far ** 2)) <= NORM, np.sqrt(np.mean(far ** 2))
     return ref
