@@ -46,7 +46,7 @@ size_t moa_cache_page_bytes(const moa_cache_desc *desc);
 /* Appends T tokens: k is turned by its position (as moa_rope_fwd) and rounded to bf16, and k and v go to the key `slot` of the
  * pool, slot = page * (keys per page) + place in the page.  q, where there is one (H > 0), is turned into q_out in the same launch.
  * q, q_out: T x H x d; k, v: T x H_kv x d, strides {token, head} in elements as in moa_rope_desc: the parts of a packed projection need
- * no copy; q_out may be q.  pos [T] int32, slot [T] int64.  A slot outside the pool (-1 for the padding of a batch) writes nothing
+ * no copy; q_out may be q, with its strides; what is written must overlap nothing else.  pos [T] int32, slot [T] int64.  A slot outside the pool (-1 for the padding of a batch) writes nothing
  * (q_out is written all the same).  The slots of one call must differ from each other; where two are the same, that key holds
  * a mixture of the two tokens.  d_rot: a multiple of 16 up to d; 0 (with H = 0; pos, inv_freq NULL): nothing is turned.
  * K's rounding is the nearest bf16 of the rotation in 64 bits, so a 4-bit page holds what quantising the bf16 page's keys would give.
@@ -79,10 +79,11 @@ moa_status moa_kv_gather(const moa_gather_desc *desc, const void *pool, const in
  * the end of a sequence does not count.
  * q: B x H x d, strides {sequence, head} as above; out [B,H,d]; lse [B,H] fp32 natural-log logsumexp of the scaled scores, may be NULL;
  * table int32, rows of max_pages entries, table_stride entries apart (0: max_pages); lens [B] int32.  dtype of q, out:
- * MOA_BF16 (fp32 scores, statistics and sums; the weights, with 4 bits their products with V's scales, are rounded once to bf16 for the
- * second product).  |scale| <= 2^60.  A page of 4 bits wants |q| < 2^59 and |v| < 2^55.  Its codes are used as numbers at the low end of bf16, against operands raised by up to
- * 2^68, so fp32's last place lies higher there: a query's product with the codes of a group is kept to 2^-84 (times the group's scale), a result's sum over 16 keys to
- * 2^-80; results below 2^-57 have fewer bits than bf16, those below 2^-80 may be 0.  A score that is NaN makes its row NaN.  Lengths are read on the device only: a captured call serves growing sequences.
+ * MOA_BF16.  Scores, statistics and sums are fp32.  Weights: bf16 pages and groups of 1 to 8, 16 bits (two bf16 pieces, a product each);
+ * groups of 9 to 16, rounded once to bf16; pages of 4 bits, the weight's product with V's scale is rounded once to bf16.  |scale| <= 2^60.  A page of 4 bits
+ * wants |q| < 2^59 and |v| < 2^55.  Its codes are used as numbers at the low end of bf16, against operands raised by up to 2^68, so fp32's last place lies higher
+ * there: a query's product with the codes of a group is kept to 2^-84 (times the group's scale), a result's sum over 16 keys to 2^-80; results below 2^-72 have fewer
+ * bits than bf16, those below 2^-80 may be 0.  A score that is NaN makes its row NaN.  Lengths are read on the device only: a captured call serves growing sequences.
  * Workspace: moa_paged_decode_workspace_bytes (partial results of sequences that several CTAs share); two calls that may
  * overlap need two. */
 typedef struct {

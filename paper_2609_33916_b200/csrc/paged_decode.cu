@@ -9,7 +9,7 @@
 //   * codes become bf16 by one mask (see `nibbles`).  K: the 8 too many are taken off in the products' starting value, -8 sum(q) of the
 //     group; V: by one packed subtraction, exact;
 //   * K's scale multiplies the products of a group of 32, in fp32; V's is multiplied into the weights, and the product rounded to bf16: the one rounding
-//     of a weight, as in the bf16 form (a weight goes there in two pieces; rounded before, too, the results are off by 0.0029 in place of 0.0023, and
+//     of a weight (it goes there in two pieces; rounded before, too, the results are off by 0.0029 in place of 0.0023, and
 //     the largest case takes 233 us in place of 241);
 //   * the page's layout (cache_layout.cuh) is the one in which a lane's codes and scales are 16-byte words: no exchange of any kind.
 // Loads.  4 bits: a fifth warp asks for the blocks of a unit by bulk copies, a lane for each of its eight blocks, with the table entries of the next four
@@ -149,6 +149,8 @@ __device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c)
 __device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ uint32_t upper(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632); }      // their upper halves
 __device__ __forceinline__ float rest(float a) { return a - __uint_as_float(__float_as_uint(a) & 0xffff0000u); }
+// The largest bf16 below a > 0 (0 for 0): what it leaves of a is not 0 either, so that both products with an infinite value are infinite
+__device__ __forceinline__ float below(float a) { return __uint_as_float((max(__float_as_uint(a), 1u) - 1u) & 0xffff0000u); }
 __device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 template <int kUnitKeys> __device__ __forceinline__ int units_of(int len) { return len > 0 ? (len + kUnitKeys - 1) / kUnitKeys : 1; }
@@ -259,6 +261,11 @@ template <int D, bool kInt4, int NQ>
 struct HeadState {
     static constexpr int kG = D / 32, kNO = D / 16, kSub = Cfg<D, kInt4, NQ>::kSub;
     static constexpr float kUp = kInt4 ? (float)kLift : 0.f;
+    // A weight as a bf16 and what that leaves, another.  4 bits: its product with V's scale is rounded once.  bf16: a product each, nothing is rounded
+    // to bf16 but the result (error against 64 bits 0.0023 -> 0.0017; B8 H32/8 n32768 160.3 -> 161.1 us, H32/4 87.4 -> 89.1).  With groups of 9 to 16, which
+    // compute for longer, that would be 8 to 13 % (B8 H32/2 n32768 53.2 -> 60.3 us): they round a weight, as 4 bits do its product (both
+    // pieces of that one: n131072 250 -> 283 us).
+    static constexpr bool kPieces = kInt4 || NQ == 1;
     uint32_t qf[NQ][kInt4 ? 4 * kG : D / 8];
     float bias[NQ][kInt4 ? kG : 1][2];      // 4 bits: the products' starting values
     float o[NQ][kNO][4], ref[NQ][2], top[NQ][2], l[NQ][2];
@@ -414,7 +421,10 @@ struct HeadState {
                 uint32_t v[4];
                 ldmatrix4_trans(v, blk + 32 * D + r * (2 * D) + ((c & ~7) | ((c ^ r) & 7)) * 16);
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) mma16816(o[n][i], v, pb[n][0], pb[n][1]);
+                for (int n = 0; n < NQ; ++n) {
+                    mma16816(o[n][i], v, pb[n][0], pb[n][1]);
+                    if constexpr (kPieces) mma16816(o[n][i], v, pr[n][0], pr[n][1]);
+                }
             }
         }
     }
@@ -472,7 +482,6 @@ struct HeadState {
                     }
                 }
         }
-        // 4 bits: a weight as its upper half and what that leaves, so that its product with V's scale is rounded once
         uint32_t pb[kSub][NQ][2], pr[kSub][NQ][2];
 #pragma unroll
         for (int s = 0; s < kSub; ++s)
@@ -482,7 +491,13 @@ struct HeadState {
                 const float p2 = ex2(fmaf(sc[s][n][2], scale, -ref[n][0])), p3 = ex2(fmaf(sc[s][n][3], scale, -ref[n][1]));
                 l[n][0] += p0 + p2;
                 l[n][1] += p1 + p3;
-                if constexpr (kInt4) {
+                if constexpr (kPieces && !kInt4) {
+                    const float h0 = below(p0), h1 = below(p1), h2 = below(p2), h3 = below(p3);
+                    pb[s][n][0] = transpose8(upper(h0, h1));
+                    pb[s][n][1] = transpose8(upper(h2, h3));
+                    pr[s][n][0] = transpose8(pack_bf16(p0 - h0, p1 - h1));
+                    pr[s][n][1] = transpose8(pack_bf16(p2 - h2, p3 - h3));
+                } else if constexpr (kPieces) {
                     pb[s][n][0] = transpose8(upper(p0, p1));
                     pb[s][n][1] = transpose8(upper(p2, p3));
                     pr[s][n][0] = transpose8(pack_bf16(rest(p0), rest(p1)));

@@ -56,7 +56,7 @@ def kernel(q, K, V, vs, table, scale, how):
             if how == "one weight for all":
                 p = np.ones_like(p)
             if vs is None:
-                w = upper_half(p) if how == "cut" else to_bf16(p)
+                w = upper_half(p) if how == "cut" else p if how == "in pieces" else to_bf16(p)
                 o = w @ v
             else:
                 f = vs[pg, j % page, kv]
@@ -83,9 +83,19 @@ def test_mistakes_do_not(four_bits, how):
     _, right = kernel(q, K, V, vs, table, 0.09, "right")
     with pytest.raises(AssertionError):
         check_paged(out, right, q, K, V, table, LENS, 0.09, four_bits, 0.5 if four_bits else 5.0)
-    if how in ("next value", "one weight for all"):        # these without the bound of the norm, too
+    if how in ("next value", "one weight for all"):        # and these in few short rows: by the bounds of the elements alone
+        b = [0, 5]
         with pytest.raises(AssertionError):
-            check_paged(out, right, q, K, V, table, LENS, 0.09, four_bits, 0.5 if four_bits else 5.0, norm=False)
+            check_paged(out[b], right[b], q[b], K, V, table[b], LENS[b], 0.09, four_bits, 0.5 if four_bits else 5.0)
+
+
+def test_a_rounded_weight_is_not_one_in_pieces():
+    q, K, V, vs, table = world(False)
+    out, lse = kernel(q, K, V, vs, table, 0.09, "in pieces")
+    check_paged(out, lse, q, K, V, table, LENS, 0.09, False, 5.0, pieces=True)
+    out, lse = kernel(q, K, V, vs, table, 0.09, "right")
+    with pytest.raises(AssertionError):
+        check_paged(out, lse, q, K, V, table, LENS, 0.09, False, 5.0, pieces=True)
 
 
 def test_a_stale_result_does_not():
@@ -93,4 +103,4 @@ def test_a_stale_result_does_not():
     out, lse = kernel(q, K, V, vs, table, 0.09, "right")
     out[1] = out[2]
     with pytest.raises(AssertionError):
-        check_paged(out, lse, q, K, V, table, LENS, 0.09, True, 0.5, norm=False)
+        check_paged(out, lse, q, K, V, table, LENS, 0.09, True, 0.5)

@@ -16,7 +16,8 @@ pytestmark = pytest.mark.gpu
 
 def check_case(c):
     K, V = oc.read_pool(c.pool.cpu().numpy(), c.page, c.Hkv, c.d, c.fmt == "int4")
-    check_paged(host(c.out), host(c.lse), host(c.q), K, V, c.table.cpu().numpy(), c.lens.cpu().numpy(), c.scale, c.fmt == "int4", 0.5 if c.fmt == "int4" else np.abs(K).max())
+    check_paged(host(c.out), host(c.lse), host(c.q), K, V, c.table.cpu().numpy(), c.lens.cpu().numpy(), c.scale, c.fmt == "int4", 0.5 if c.fmt == "int4" else np.abs(K).max(),
+                pieces=c.fmt == "bf16" and c.H // c.Hkv <= 8)
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "int4"])
@@ -36,6 +37,25 @@ def test_values_of_one_sign(width):
     v.copy_(0x99 + (v & 0x66))
     c.run()
     check_case(c)
+
+
+@pytest.mark.parametrize("H,Hkv", [(1, 1), (4, 1), (8, 1), (12, 1)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_infinite_values(d, H, Hkv):
+    """A value that is infinite makes its element infinite, whatever bits its weight has (a key alone: a weight of 1); the others are what they are."""
+    lens = [1, 2, 3, 16, 17, 40, 130]
+    c = Case("bf16", lens, H, Hkv, d, 16, scale=0.05, seed=42)
+    c.run()
+    want = c.out.clone()
+    rows = c.pool.view(torch.bfloat16).view(c.pages, Hkv, 2, 16, d)
+    for b, n in enumerate(lens):
+        j = n // 2
+        rows[c.table[b, j // 16].long(), :, 1, j % 16, 5] = float("inf")
+        rows[c.table[b, j // 16].long(), :, 1, j % 16, d - 9] = float("-inf")
+    out, _ = c.run(out=torch.zeros_like(c.out))
+    assert bool(torch.isposinf(out[..., 5]).all()) and bool(torch.isneginf(out[..., d - 9]).all())
+    rest = [i for i in range(d) if i not in (5, d - 9)]
+    assert torch.equal(out[..., rest], want[..., rest])
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "int4"])
@@ -97,4 +117,5 @@ def test_a_served_batch_key_by_key(fmt, H, Hkv, d):
             for got, x0 in ((K, k), (V, host(y[:, H + Hkv:]))):
                 np.testing.assert_array_equal(got[p // page, p % page], oc.value4(*oc.quantise(x0)) if fmt == "int4" else x0)
             most = max(most, np.abs(K[p // page, p % page]).max())
-        check_paged(host(out), host(lse), host(q1), K, V, table.cpu().numpy(), n, d ** -0.5, fmt == "int4", most / 7 if fmt == "int4" else most)
+        check_paged(host(out), host(lse), host(q1), K, V, table.cpu().numpy(), n, d ** -0.5, fmt == "int4", most / 7 if fmt == "int4" else most,
+                    pieces=fmt == "bf16" and H // Hkv <= 8)
