@@ -4,7 +4,9 @@
     "linear"  positions divided by `factor`: inv_freq / factor
     "ntk"     a larger base, base * factor^(d_rot / (d_rot - 2)): the lowest frequency is divided by the factor, the highest stays
     "yarn"    by how often a pair turns over the length that was trained on: pairs that turn more than beta_fast times stay, pairs that turn less than
-              beta_slow times are divided by the factor, those between are blended; the rotated q and k are multiplied by 0.1 ln(factor) + 1
+              beta_slow times are divided by the factor, those between are blended, linearly in the number of turns (the published form; where a model
+              was trained with a ramp in the pair's index, between rounded limits, its frequencies are passed to the kernels as they are); the
+              rotated q and k are multiplied by 0.1 ln(factor) + 1
 """
 from __future__ import annotations
 
