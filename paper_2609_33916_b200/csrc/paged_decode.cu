@@ -95,26 +95,13 @@ __device__ __forceinline__ uint2 lds64(uint32_t a)
     asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
     return v;
 }
-__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
     uint32_t y;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// The same from a starting value of its own: rows g and g + 8 begin at (c0, c1)
+// mma16816 from a starting value of its own: rows g and g + 8 begin at (c0, c1)
 __device__ __forceinline__ void mma16816_from(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
@@ -661,7 +648,7 @@ __device__ __forceinline__ void write_result(const PagedArgs &a, int head, int g
 template <int D, class C>
 __device__ __forceinline__ void last_joins(const PagedArgs &a, int team, int head, int ca, int cb, unsigned int *flag)
 {
-    constexpr int kJoin = 32 * kWarps, kBatch = 4;
+    constexpr int kJoin = 32 * kWarps;
     const int tid = threadIdx.x % kJoin;
     // the fences of the thread that counts order what the barriers in front of and behind it have gathered: the team's part before the count, the
     // other teams' parts, if it is the last, before the reads
@@ -675,36 +662,7 @@ __device__ __forceinline__ void last_joins(const PagedArgs &a, int team, int hea
     if (*flag != (unsigned)(cb - ca)) return;
     for (int idx = tid; idx < a.G * (D / 4); idx += kJoin) {
         const int g = idx / (D / 4), c = 4 * (idx % (D / 4));
-        float mt = -INFINITY, ls = 0.f;
-        float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k0 = ca; k0 <= cb; k0 += kBatch) {
-            float2 ml[kBatch];
-            float4 v[kBatch];
-            float mn = mt;
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const size_t at = (size_t)(2 * (k0 + u) + (k0 + u == ca ? 1 : 0)) * a.G + g;
-                const bool there = k0 + u <= cb;
-                ml[u] = there ? __ldcg(reinterpret_cast<const float2 *>(a.part_ml + at * 2)) : make_float2(-INFINITY, 0.f);
-                v[u] = there ? __ldcg(reinterpret_cast<const float4 *>(a.part_o + at * D + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, ml[u].x);
-            const float ref = mn == -INFINITY ? 0.f : mn, b = ex2(mt - ref);
-            mt = mn;
-            ls *= b;
-            ot.x *= b; ot.y *= b; ot.z *= b; ot.w *= b;
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const float f = ex2(ml[u].x - ref);
-                ls = fmaf(ml[u].y, f, ls);
-                ot.x = fmaf(v[u].x, f, ot.x); ot.y = fmaf(v[u].y, f, ot.y); ot.z = fmaf(v[u].z, f, ot.z); ot.w = fmaf(v[u].w, f, ot.w);
-            }
-        }
-        const size_t at = (size_t)head * a.G + g;
-        const float inv = ls == 0.f ? 0.f : 1.f / ls;
-        *reinterpret_cast<uint2 *>(a.out + at * D + c) = make_uint2(pack_bf16(ot.x * inv, ot.y * inv), pack_bf16(ot.z * inv, ot.w * inv));
-        if (a.lse && c == 0) a.lse[at] = ls == 0.f ? -INFINITY : (mt + __log2f(ls)) * kLn2;
+        write_result<D>(a, head, g, c, join_parts<D, 1, 4>(a, g, c, cb - ca + 1, 0, [&](int k) { return 2 * (ca + k) + (k == 0 ? 1 : 0); }));
     }
 }
 

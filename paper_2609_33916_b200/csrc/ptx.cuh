@@ -623,6 +623,21 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
+// Warp-level tiles: four 8 x 8 matrices of 16 bits from shared memory, and the product of 16 rows (a), 16 terms and 8 columns (b)
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
 // Backward: r[e] = r[e] * sl2 + Ls[e] (a row of S^T in place; Ls = -L log2 e in shared memory, 16-byte aligned), the argument of exp2, and where
 // `masked` -inf for the queries e < first, which do not see this key.  The mask stands in a branch of its own: written beside each
 // exponential it was two instructions per score in every tile, masked or not.  (Behind the addition of L, so that a masked P is 0 whatever L is.)
